@@ -335,6 +335,72 @@ int moe_layer_forward(moe_ctx* ctx, const moe_layer_args* args, const moe_policy
 int moe_ep_segments(moe_ctx* ctx, const int32_t* recv_counts, int32_t W, int32_t E_loc,
                     int32_t* seg_offsets, int32_t* seg_expert, void* stream);
 
+/* ---- Experts kept in 4 bits, and gradients of the layer ----
+ * Serving a few tokens reads little but expert weights; these calls keep them in 4 bits.  The gradients train what feeds the layer
+ * and its router, through experts that stay as they are:
+ *     moe_combine_backward -> moe_expert_ffn_mx4_backward -> moe_route_backward
+ * are the gradients of moe_combine, moe_expert_ffn_mx4 and moe_route (moe_gate + moe_dispatch).  A gradient's buffers do not
+ * overlap its inputs.  Sums run in float in a fixed order (no atomics): equal calls give equal bits.
+ *
+ * Format (OCP MXFP4): weight row n of a [rows][cols] array holds cols / 2 bytes of codes, column 2c in the low and column 2c + 1 in
+ * the high half of byte c, and cols / 32 scale bytes, one per 32 columns.  Codes 0..7 stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 is the sign;
+ * scale byte b stands for 2^(b - 127), 255 for NaN.  Expert arrays are W1_codes[E][F][d/2], W1_scales[E][F][d/32],
+ * W2_codes[E][d][F/2], W2_scales[E][d][F/32] (E + n_shared experts with shared ones). */
+
+/* W[rows][cols] (dtype) to codes and scales: the scale of a group is the smallest power of two s >= 2^-126 with max|w| <= 7 s (larger
+ * magnitudes than 6 s round to 6 s, no further off than the spacing there allows), a code is the nearest to w / s, ties to the even code.
+ * A group that holds infinity or NaN gets scale byte 255 and codes 0.  values (dtype, may be NULL) receives what the codes stand for,
+ * for training that sees the quantisation or for its error.
+ *   rows >= 0, cols a multiple of 32, rows * cols <= 2^38; all of an expert array at once: rows = E * F */
+int moe_quantize_mx4(moe_ctx* ctx, const void* W, int64_t rows, int32_t cols, uint8_t* codes, uint8_t* scales, void* values,
+                     void* stream);
+
+/* moe_expert_ffn on 4-bit weights: u = W1_e . x + b1_e, h = W2_e . gelu(u) + b2_e for every row of every segment.  The weights
+ * are exact in the products (a code with its scale is a bf16 value); sums are float, and gelu(u) is rounded to dtype once.
+ *   in : x_rows: packed rows (row_pairs NULL) or x[T][d] read through row_pairs as in moe_expert_ffn_rows;
+ *        out_pairs: NULL, or the row of h_rows that packed row r goes to (distinct), as in moe_expert_ffn_commit: with
+ *        moe_dispatch's perm and h_rows = H_cache, moe_combine with h_packed = NULL follows;
+ *        seg_offsets, seg_expert, n_segments, max_rows, b1, b2 as in moe_expert_ffn.  Packed rows from max_rows on are not
+ *        touched (moe_expert_ffn_status reports that there were some), nor are segments whose expert is out of range
+ *   out: h_rows (dtype); u_packed[..][F] (dtype, may be NULL): the pre-activations by packed row, for the gradient
+ * workspace: moe_workspace_bytes().  d and F multiples of 32, at most 2^20. */
+int moe_expert_ffn_mx4(moe_ctx* ctx, const void* x_rows, const int32_t* row_pairs, const int32_t* out_pairs,
+                       const int32_t* seg_offsets, const int32_t* seg_expert, int32_t n_segments, int32_t max_rows,
+                       const uint8_t* W1_codes, const uint8_t* W1_scales, const float* b1, const uint8_t* W2_codes,
+                       const uint8_t* W2_scales, const float* b2, void* u_packed, void* h_rows, void* workspace, void* stream);
+
+/* Gradient of moe_expert_ffn_mx4 with respect to its rows: du = (dh . W2_e) gelu'(u), dx = du . W1_e, by packed row.
+ *   in : dh_packed[..][d], u_packed[..][F] as the forward call left it; the segments and weights of that call
+ *   out: dx_packed[..][d]; du_packed[..][F] (may be NULL, kept in the workspace then): the gradient of u, rounded to dtype,
+ *        which dx is formed from (its sums over a segment's rows are the gradient of b1)
+ * Rows outside every segment and from max_rows on are not touched. */
+int moe_expert_ffn_mx4_backward(moe_ctx* ctx, const void* dh_packed, const void* u_packed, const int32_t* seg_offsets,
+                                const int32_t* seg_expert, int32_t n_segments, int32_t max_rows, const uint8_t* W1_codes,
+                                const uint8_t* W1_scales, const uint8_t* W2_codes, const uint8_t* W2_scales, void* du_packed,
+                                void* dx_packed, void* workspace, void* stream);
+
+/* Gradient of moe_combine without caches (y_i = sum_j scores_ij h_ij over the pairs that have a packed row):
+ *   dh_packed[inv[p]] = scores[p] dy_i (rounded once), dscores[p] = <h_packed[inv[p]], dy_i>, 0 for pairs with inv[p] = -1.
+ *   in : dy[T][d], h_packed[R][d] (dtype), inv[T*k], scores[T][k]      out: dh_packed[R][d] (dtype), dscores[T][k] float
+ * With shared experts their columns of dscores are written like the others (moe_route_backward does not read them). */
+int moe_combine_backward(moe_ctx* ctx, const void* dy, const void* h_packed, const int32_t* inv, const float* scores, int32_t T,
+                         void* dh_packed, float* dscores, void* stream);
+
+/* Gradient of moe_gate and moe_dispatch together: with z the logits and P = probs_all their softmax,
+ *   dz   = what dscores (the routed columns), dprobs (gradient of probs_all, may be NULL) and dlogits (gradient of the logits
+ *          themselves, may be NULL) give for z; with renorm_topk through the division by the selected sum; the selection is constant
+ *   dx_i = sum over the slots j of dx_packed[inv_ij] (pairs with -1 left out; in slot order, then the router's share)
+ *          + sum_e dz_ie Wg_e,      dWg = dz^T x,      dbg = sum_i dz_i
+ *   in : x[T][d], Wg[E][d] (dtype), expert_idx[T][k], probs_all[T][E] of moe_gate, dscores[T][k];
+ *        dx_packed[R][d] (dtype) with inv[T*k], or both NULL: the router alone
+ *   out: dx[T][d] (dtype); dz[T][E], dWg[E][d], dbg[E] float, each may be NULL (x may be NULL without dWg)
+ * Wg NULL: the gradient of the dispatch alone (x_packed -> x, also what returns to a token's home under expert parallelism);
+ * only dx_packed, inv and dx are used then, and dz, dWg and dbg have to be NULL.
+ * workspace: moe_workspace_bytes() (not used without Wg).  T = 0 writes zeros to dWg and dbg. */
+int moe_route_backward(moe_ctx* ctx, const void* x, const void* Wg, const int32_t* expert_idx, const float* probs_all,
+                       const float* dscores, const float* dprobs, const float* dlogits, const void* dx_packed, const int32_t* inv,
+                       int32_t T, void* dx, float* dz, float* dWg, float* dbg, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

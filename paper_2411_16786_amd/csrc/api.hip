@@ -45,13 +45,15 @@ size_t hidden_bytes(const moe_ctx* ctx)
 }
 
 // the two status words of the FFN's launch check sit behind the hidden activations and the partial sums
-// (the dispatch scratch shares the start of the workspace with the hidden activations: the calls of one
-// workspace run in stream order)
+// (the dispatch scratch and the partial sums of moe_route_backward share the start of the workspace with the
+// hidden activations: the calls of one workspace run in stream order)
 size_t status_offset(const moe_ctx* ctx)
 {
     size_t front = hidden_bytes(ctx);
     const size_t disp = dicemoe::dispatch_scratch_bytes(static_cast<long long>(ctx->shape.T_max) * slots(ctx), experts(ctx));
     if (disp > front) front = (disp + 255) / 256 * 256;
+    const size_t route = dicemoe::route_backward_bytes(ctx->shape.T_max, ctx->shape.E, ctx->shape.d);
+    if (route > front) front = (route + 255) / 256 * 256;
     return front + (is_bf16(ctx) ? dicemoe::kSplitKBytes : 0);
 }
 
@@ -181,6 +183,18 @@ int check_ffn(moe_ctx* ctx, const char* who, const void* x_rows, const int32_t* 
     if (!workspace) {
         std::snprintf(ctx->err, sizeof(ctx->err), "%s: workspace is null", who);
         return MOE_ERR_WORKSPACE;
+    }
+    return MOE_OK;
+}
+
+// The 4-bit expert FFN calls: whole scale groups in every weight row, offsets inside one expert's codes well within 64 bits, and a
+// launch of at most 2^31 workgroups
+int check_mx4(moe_ctx* ctx, const char* who)
+{
+    const moe_shape& s = ctx->shape;
+    if (s.d % 32 != 0 || s.F % 32 != 0 || s.d > (1 << 20) || s.F > (1 << 20)) {
+        std::snprintf(ctx->err, sizeof(ctx->err), "%s: d=%d and F=%d have to be multiples of 32 up to 2^20", who, s.d, s.F);
+        return MOE_ERR_SHAPE;
     }
     return MOE_OK;
 }
@@ -534,6 +548,91 @@ int moe_layer_forward(moe_ctx* ctx, const moe_layer_args* a, const moe_policy* p
                                               ctx->shape.k, H_cache, S_cache, use_fresh, a->y, static_cast<hipStream_t>(stream)),
                           "moe_layer_forward");
     return moe_combine(ctx, h_packed, a->inv, a->scores, mask, a->T, H_cache, S_cache, use_fresh, a->y, stream);
+}
+
+int moe_quantize_mx4(moe_ctx* ctx, const void* W, int64_t rows, int32_t cols, uint8_t* codes, uint8_t* scales, void* values, void* stream)
+{
+    if (!ctx) return MOE_ERR_NULL;
+    if (rows < 0 || cols < 32 || cols % 32 != 0 || rows > (1ll << 38) / cols)
+        return fail(ctx, MOE_ERR_SHAPE, "moe_quantize_mx4: rows=%ld, cols=%ld (cols a multiple of 32, rows * cols up to 2^38)", static_cast<long>(rows), cols);
+    if (rows == 0) return MOE_OK;
+    if (!W || !codes || !scales) return fail(ctx, MOE_ERR_NULL, "moe_quantize_mx4: null pointer");
+    return hip_result(ctx, launch_quantize_mx4(is_bf16(ctx), W, rows, cols, codes, scales, values, static_cast<hipStream_t>(stream)), "moe_quantize_mx4");
+}
+
+int moe_expert_ffn_mx4(moe_ctx* ctx, const void* x_rows, const int32_t* row_pairs, const int32_t* out_pairs, const int32_t* seg_offsets,
+                       const int32_t* seg_expert, int32_t n_segments, int32_t max_rows, const uint8_t* W1_codes, const uint8_t* W1_scales,
+                       const float* b1, const uint8_t* W2_codes, const uint8_t* W2_scales, const float* b2, void* u_packed, void* h_rows,
+                       void* workspace, void* stream)
+{
+    const char* const who = "moe_expert_ffn_mx4";
+    if (!ctx) return MOE_ERR_NULL;
+    if (int rc = check_mx4(ctx, who)) return rc;
+    if (max_rows == 0) x_rows = h_rows = workspace;      // no row is read or written: an empty tensor's null will do
+    if (int rc = check_ffn(ctx, who, x_rows, seg_offsets, seg_expert, n_segments, max_rows, W1_codes, W2_codes, h_rows, workspace)) return rc;
+    if (!W1_scales || !W2_scales) return fail(ctx, MOE_ERR_NULL, "moe_expert_ffn_mx4: scales are null");
+    const moe_shape& s = ctx->shape;
+    const Segments seg = {seg_offsets, seg_expert, n_segments, experts(ctx), max_rows};
+    int32_t* const status = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + status_offset(ctx));
+    return hip_result(ctx,
+                      launch_expert_ffn_mx4(is_bf16(ctx), x_rows, row_pairs, slots(ctx), seg, s.d, s.F, {W1_codes, W1_scales}, b1,
+                                            {W2_codes, W2_scales}, b2, u_packed, h_rows, out_pairs, workspace, status, static_cast<hipStream_t>(stream)),
+                      who);
+}
+
+int moe_expert_ffn_mx4_backward(moe_ctx* ctx, const void* dh_packed, const void* u_packed, const int32_t* seg_offsets,
+                                const int32_t* seg_expert, int32_t n_segments, int32_t max_rows, const uint8_t* W1_codes,
+                                const uint8_t* W1_scales, const uint8_t* W2_codes, const uint8_t* W2_scales, void* du_packed,
+                                void* dx_packed, void* workspace, void* stream)
+{
+    const char* const who = "moe_expert_ffn_mx4_backward";
+    if (!ctx) return MOE_ERR_NULL;
+    if (int rc = check_mx4(ctx, who)) return rc;
+    if (max_rows == 0) dh_packed = u_packed = dx_packed = workspace;
+    if (int rc = check_ffn(ctx, who, dh_packed, seg_offsets, seg_expert, n_segments, max_rows, W1_codes, W2_codes, dx_packed, workspace)) return rc;
+    if (!u_packed || !W1_scales || !W2_scales) return fail(ctx, MOE_ERR_NULL, "moe_expert_ffn_mx4_backward: null pointer");
+    const moe_shape& s = ctx->shape;
+    const Segments seg = {seg_offsets, seg_expert, n_segments, experts(ctx), max_rows};
+    int32_t* const status = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + status_offset(ctx));
+    return hip_result(ctx,
+                      launch_expert_ffn_mx4_backward(is_bf16(ctx), dh_packed, u_packed, seg, s.d, s.F, {W1_codes, W1_scales},
+                                                     {W2_codes, W2_scales}, du_packed ? du_packed : workspace, dx_packed, status,
+                                                     static_cast<hipStream_t>(stream)),
+                      who);
+}
+
+int moe_combine_backward(moe_ctx* ctx, const void* dy, const void* h_packed, const int32_t* inv, const float* scores, int32_t T,
+                         void* dh_packed, float* dscores, void* stream)
+{
+    if (!ctx) return MOE_ERR_NULL;
+    if (int rc = check_T(ctx, T)) return rc;
+    if (T == 0) return MOE_OK;
+    if (!dy || !h_packed || !inv || !scores || !dh_packed || !dscores) return fail(ctx, MOE_ERR_NULL, "moe_combine_backward: null pointer");
+    return hip_result(ctx,
+                      launch_combine_backward(is_bf16(ctx), dy, h_packed, inv, scores, T, ctx->shape.d, slots(ctx), dh_packed, dscores,
+                                              static_cast<hipStream_t>(stream)),
+                      "moe_combine_backward");
+}
+
+int moe_route_backward(moe_ctx* ctx, const void* x, const void* Wg, const int32_t* expert_idx, const float* probs_all, const float* dscores,
+                       const float* dprobs, const float* dlogits, const void* dx_packed, const int32_t* inv, int32_t T, void* dx,
+                       float* dz, float* dWg, float* dbg, void* workspace, void* stream)
+{
+    if (!ctx) return MOE_ERR_NULL;
+    if (int rc = check_T(ctx, T)) return rc;
+    const bool rows = T > 0;                             // without tokens only dWg and dbg are written, whatever the other pointers are
+    if (rows && (!dx || (dx_packed == nullptr) != (inv == nullptr))) return fail(ctx, MOE_ERR_NULL, "moe_route_backward: null pointer");
+    const moe_shape& s = ctx->shape;
+    if (Wg) {
+        if (rows && (!expert_idx || !probs_all || !dscores || (dWg && !x))) return fail(ctx, MOE_ERR_NULL, "moe_route_backward: null pointer");
+        if (static_cast<long long>(s.E) * s.d >= (1ll << 31)) return fail(ctx, MOE_ERR_SHAPE, "moe_route_backward: E * d beyond 2^31");
+        if (!workspace) return fail(ctx, MOE_ERR_WORKSPACE, "moe_route_backward: workspace is null");
+    } else if ((rows && !dx_packed) || dz || dWg || dbg) {
+        return fail(ctx, MOE_ERR_NULL, "moe_route_backward: without Wg it is the gradient of the dispatch alone, which needs dx_packed and inv and gives dx");
+    }
+    const RouteBackward a = {x, Wg, expert_idx, probs_all, dscores, dprobs, dlogits, dx_packed, inv, dx, dz, dWg, dbg,
+                             T, s.d, s.E, s.k, slots(ctx), s.renorm_topk, nullptr, nullptr};
+    return hip_result(ctx, launch_route_backward(is_bf16(ctx), a, workspace, static_cast<hipStream_t>(stream)), "moe_route_backward");
 }
 
 int moe_ep_segments(moe_ctx* ctx, const int32_t* recv_counts, int32_t W, int32_t E_loc, int32_t* seg_offsets,

@@ -93,6 +93,41 @@ hipError_t launch_commit_scores(const float* scores, const uint8_t* mask, int T_
 hipError_t launch_calibrate_copy(void* dst, const void* src, size_t bytes, int workgroups, hipStream_t stream);
 hipError_t launch_calibrate_mfma(const void* operands, float* sink, int iters, int workgroups, hipStream_t stream);
 
+// W[rows][cols] -> 4-bit codes [rows][cols / 2], scale bytes [rows][cols / 32] and (values not null) what they stand for, dtype
+hipError_t launch_quantize_mx4(bool bf16, const void* W, long long rows, int cols, uint8_t* codes, uint8_t* scales, void* values,
+                               hipStream_t stream);
+
+// One expert weight array in 4 bits: codes [experts][rows][cols / 2], scales [experts][rows][cols / 32]
+struct Mx4 { const uint8_t* codes; const uint8_t* scales; };
+// The rows of a grouped product and where they belong.  Rows at and beyond max_rows are not touched.
+struct Segments { const int32_t* offsets; const int32_t* expert; int n, n_experts, max_rows; };
+// launch_expert_ffn on 4-bit weights; pre (may be null) receives the pre-activations [rows][F]
+hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
+                                 const Mx4& W1, const float* b1, const Mx4& W2, const float* b2, void* pre, void* h_out,
+                                 const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream);
+// du = (dh W2) gelu'(u), dx = du W1, row by row of the packed order
+hipError_t launch_expert_ffn_mx4_backward(bool bf16, const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1,
+                                          const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream);
+
+hipError_t launch_combine_backward(bool bf16, const void* dy, const void* h_packed, const int32_t* inv, const float* scores, int T_tok,
+                                   int d, int k, void* dh_packed, float* dscores, hipStream_t stream);
+
+// Gradient of router and dispatch (Wg null: of the dispatch alone).  slots: columns of idx, dscores and inv, the first k of them routed.
+// partial, partial_dbg: set by the launcher, in a workspace of route_backward_bytes(T, E, d) bytes.
+struct RouteBackward {
+    const void *x, *Wg;
+    const int32_t* idx;
+    const float *probs, *dscores, *dprobs, *dlogits;
+    const void* dx_packed;
+    const int32_t* inv;
+    void* dx;
+    float *dz, *dWg, *dbg;
+    int T, d, E, k, slots, renorm;
+    float *partial, *partial_dbg;
+};
+size_t route_backward_bytes(long long T_max, int E, int d);
+hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hipStream_t stream);
+
 hipError_t launch_ep_segments(const int32_t* recv_counts, int n_seg, int E_loc, int32_t* seg_offsets,
                               int32_t* seg_expert, hipStream_t stream);
 

@@ -1,0 +1,314 @@
+// Expert FFN on 4-bit weights (mx4.hpp), forward and gradient of its rows, as grouped products over segments of rows.
+//   forward : u = x W1_e^T + b1_e,   h = gelu(u) W2_e^T + b2_e        (gelu(u) rounded to the storage type once)
+//   gradient: du = (dh W2_e) gelu'(u),   dx = du W1_e                 (du rounded to the storage type once)
+// The weights are the first operand of the matrix instructions and the rows the second, so a result register holds four
+// output columns of one row.  Weights go from memory to the instruction through registers alone, converted on the way.
+#include <type_traits>
+#include "ffn_mfma.hpp"
+#include "kernels.hpp"
+#include "mx4.hpp"
+
+namespace dicemoe {
+
+// Phi(-a) for a in 0 .. 6: the polynomial that gelu_erf_fast has in its body
+__device__ __forceinline__ float normal_tail(float a) {
+    float p = fmaf(0x1.159ab2p-15f, a, -0x1.934b26p-11f);
+    p = fmaf(p, a, 0x1.08ca02p-7f);
+    p = fmaf(p, a, -0x1.b58d52p-5f);
+    p = fmaf(p, a, -0x1.d5c80ep-2f);
+    p = fmaf(p, a, -0x1.26b528p+0f);
+    p = fmaf(p, a, -0x1.ffff18p-1f);
+    return __builtin_amdgcn_exp2f(p);
+}
+// gelu and its slope.  The bf16 forms use that polynomial; NaN stays NaN in all of them.
+template <typename T> __device__ __forceinline__ float mx4_gelu(float u);
+template <> __device__ __forceinline__ float mx4_gelu<float>(float u) { return gelu_erf(u); }
+template <> __device__ __forceinline__ float mx4_gelu<bf16_t>(float u) { return u != u ? u : gelu_erf_fast(u); }
+// gelu'(u) = Phi(u) + u phi(u); with a = |u| it is 1 - s for u >= 0 and s below, s = Phi(-a) - a phi(a)
+template <typename T> __device__ __forceinline__ float gelu_slope(float u);
+template <> __device__ __forceinline__ float gelu_slope<float>(float u) {
+    return 0.5f * (1.0f + erff(u * 0.70710678118654752440f)) + u * (0.39894228040143267794f * expf(-0.5f * u * u));
+}
+template <> __device__ __forceinline__ float gelu_slope<bf16_t>(float u) {
+    const float a = fminf(fabsf(u), 6.0f);
+    const float bell = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * a * a);
+    const float s = normal_tail(a) - a * bell;
+    return u != u ? u : (u >= 0.0f ? 1.0f - s : s);
+}
+
+// The segment that row tile `tile` (BM rows, tiles of a segment contiguous) belongs to, found 64 segments at a time by lanes; all lanes
+// of a wavefront get the same answer.  Rows from max_rows on and segments of no known expert have no tiles.
+__device__ __forceinline__ bool find_tile(const Segments& s, int BM, int tile, int& expert, int& row0, int& row_end)
+{
+    const int lane = lane_id();
+    for (int base = 0; base < s.n; base += kWave) {
+        int begin = 0, end = 0, e = -1;
+        if (base + lane < s.n) {
+            begin = s.offsets[base + lane];
+            end = s.offsets[base + lane + 1];
+            e = s.expert[base + lane];
+            end = end < s.max_rows ? end : s.max_rows;
+        }
+        const bool used = end > begin && begin >= 0 && e >= 0 && e < s.n_experts;
+        const int upto = wave_scan(used ? (end - begin + BM - 1) / BM : 0);     // tiles of the lanes up to this one
+        const uint64_t past = __ballot(upto > tile);
+        if (past != 0) {
+            const int src = __ffsll(static_cast<unsigned long long>(past)) - 1;
+            const int before = src > 0 ? __builtin_amdgcn_readlane(upto, src - 1) : 0;
+            expert = __builtin_amdgcn_readlane(e, src);
+            row0 = __builtin_amdgcn_readlane(begin, src) + (tile - before) * BM;
+            row_end = __builtin_amdgcn_readlane(end, src);
+            return true;
+        }
+        tile -= __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    return false;
+}
+
+__device__ __forceinline__ void store4(bf16_t* p, const float* v) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+__device__ __forceinline__ void store4(float* p, const float* v) {
+    *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+}
+
+// Forward product of few rows: out[r, n] = act(sum_k x[r, k] W_e[n, k] + b[n]).  A workgroup takes 16 rows and 16 NT columns n; its KS
+// wavefronts share out the reduction in steps of 128 and meet in LDS.  Lane (g, m) = (l / 16, l % 16) loads the 16 bytes of
+// codes, the scale and the row's values of k = 128 s + 32 g .. + 31 for its row of weights and its row of x: a lane's 16 bytes are
+// exactly one scale group.  The order of k inside a step does not matter as long as both operands have the same.
+// Bound by the weights' bytes and, with few of them, by one trip to memory: a wavefront asks for everything of a step at once.
+template <typename T, int NT, int KS, bool GELU>
+__global__ __launch_bounds__(KS * kWave) void mx4_rows_kernel(const T* __restrict__ x, const int32_t* __restrict__ row_index, int row_div,
+                                                              Segments seg, int N, int K, Mx4 W, const float* __restrict__ bias,
+                                                              T* __restrict__ pre, T* __restrict__ out,
+                                                              const int32_t* __restrict__ out_index, int32_t* __restrict__ status)
+{
+    constexpr int XV = 32 / Store<T>::kVec;                     // 16-byte loads of a row per step
+    __shared__ f32x4_t red[KS][NT][kWave];
+    report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
+    const int n_blocks = (N + 16 * NT - 1) / (16 * NT);
+    const int tile = blockIdx.x / n_blocks, nb = (blockIdx.x - tile * n_blocks) * 16 * NT;
+    int expert, row0, row_end;
+    if (!find_tile(seg, 16, tile, expert, row0, row_end)) return;
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int m = lane & 15, g = lane >> 4;
+
+    const int r = row0 + m < row_end ? row0 + m : row_end - 1;  // rows past the end repeat the last; never stored
+    const T* const xr = x + static_cast<size_t>(row_index ? row_index[r] / row_div : r) * K;
+    const uint8_t *wc[NT], *ws[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        int n = nb + (m >> 2) * 4 * NT + t * 4 + (m & 3);       // result registers of a lane: 4 NT consecutive columns
+        n = n < N ? n : N - 1;
+        const size_t row = static_cast<size_t>(expert) * N + n;
+        wc[t] = W.codes + row * (K / 2);
+        ws[t] = W.scales + row * (K / kMxGroup);
+    }
+    f32x4_t acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int k0 = wave * 128; k0 < K; k0 += KS * 128) {
+        const int k = k0 + g * 32;
+        const bool on = k < K;
+        u32x4_t c[NT], xv[XV];
+        float s[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            c[t] = on ? *reinterpret_cast<const u32x4_t*>(wc[t] + k / 2) : u32x4_t{0u, 0u, 0u, 0u};
+            s[t] = mx4_scale(on ? ws[t][k / kMxGroup] : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < XV; ++i) xv[i] = on ? *reinterpret_cast<const u32x4_t*>(xr + k + i * Store<T>::kVec) : u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {                       // eight codes
+                if constexpr (sizeof(T) == 2) {
+                    const u32x4_t a = {mx4_bf16<0>(c[t][q], s[t]), mx4_bf16<1>(c[t][q], s[t]), mx4_bf16<2>(c[t][q], s[t]), mx4_bf16<3>(c[t][q], s[t])};
+                    acc[t] = RowMfma<bf16_t>::step(a, xv[q], acc[t], 0);
+                } else {
+                    const f32x2_t p0 = mx4_f32<0>(c[t][q], s[t]), p1 = mx4_f32<1>(c[t][q], s[t]), p2 = mx4_f32<2>(c[t][q], s[t]), p3 = mx4_f32<3>(c[t][q], s[t]);
+                    const float a[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], __uint_as_float(xv[2 * q + i / 4][i % 4]), acc[t], 0, 0, 0);
+                }
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) red[wave][t][lane] = acc[t];
+    __syncthreads();
+    for (int t = wave; t < NT; t += KS) {
+        f32x4_t sum = red[0][t][lane];
+#pragma unroll
+        for (int w = 1; w < KS; ++w) sum += red[w][t][lane];
+        const int n = nb + g * 4 * NT + t * 4;
+        if (row0 + m >= row_end || n >= N) continue;
+        if (bias) sum += *reinterpret_cast<const f32x4_t*>(bias + static_cast<size_t>(expert) * N + n);
+        float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+        if (pre) store4(pre + static_cast<size_t>(r) * N + n, v);
+        if (GELU) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = mx4_gelu<T>(v[i]);
+        }
+        store4(out + static_cast<size_t>(out_index ? out_index[r] : r) * N + n, v);
+    }
+}
+
+// Transposed product of few rows, for the gradient: out[r, k] = sum_n y[r, n] W_e[n, k], times gelu'(u[r, k]) with SLOPE.  A workgroup
+// takes 16 rows and 128 columns k; its four wavefronts share out the reduction in steps of 32 rows of weights.  Lane (g, m) loads, for n =
+// 32 s + 8 g + q (q = 0 .. 7), the dword of codes of columns k = kb + 8 m .. + 7 and their scale; matrix instruction i takes column i
+// of every lane's eight, i.e. its result row 4 g + v stands for column kb + 32 g + 8 v + i.  In bf16 a conversion gives two columns of
+// one n, and pairs along n are put together by byte permutation: one conversion and one permutation per two weights.
+template <typename T, bool SLOPE>
+__global__ __launch_bounds__(256) void mx4_rows_transposed_kernel(const T* __restrict__ y, Segments seg, int N, int K, Mx4 W,
+                                                                  const T* __restrict__ u, T* __restrict__ out, int32_t* __restrict__ status)
+{
+    constexpr int KS = 4, YV = 8 / Store<T>::kVec;
+    __shared__ f32x4_t red[KS][8][kWave];
+    report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
+    const int k_blocks = (K + 127) / 128;
+    const int tile = blockIdx.x / k_blocks, kb = (blockIdx.x - tile * k_blocks) * 128;
+    int expert, row0, row_end;
+    if (!find_tile(seg, 16, tile, expert, row0, row_end)) return;
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int m = lane & 15, g = lane >> 4;
+    const int r = row0 + m < row_end ? row0 + m : row_end - 1;
+    const int k = kb + m * 8;
+    const bool on = k < K;
+    const size_t first = static_cast<size_t>(expert) * N + g * 8;
+    const uint8_t* const wc = W.codes + first * (K / 2) + (on ? k / 2 : 0);
+    const uint8_t* const ws = W.scales + first * (K / kMxGroup) + (on ? k / kMxGroup : 0);
+    const T* const yr = y + static_cast<size_t>(r) * N + g * 8;
+    f32x4_t acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int n0 = wave * 32; n0 < N; n0 += KS * 32) {
+        uint32_t c[8];
+        float s[8];
+        u32x4_t yv[YV];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {                           // (columns past the end repeat the first; never stored)
+            c[q] = *reinterpret_cast<const uint32_t*>(wc + static_cast<size_t>(n0 + q) * (K / 2));
+            s[q] = mx4_scale(ws[static_cast<size_t>(n0 + q) * (K / kMxGroup)]);
+        }
+#pragma unroll
+        for (int i = 0; i < YV; ++i) yv[i] = *reinterpret_cast<const u32x4_t*>(yr + n0 + i * Store<T>::kVec);
+        auto columns = [&](auto B) {                            // columns 2 B and 2 B + 1
+            constexpr int b = decltype(B)::value;
+            if constexpr (sizeof(T) == 2) {
+                u32x4_t lo, hi;
+#pragma unroll
+                for (int q = 0; q < 8; q += 2) {
+                    const uint32_t p0 = mx4_bf16<b>(c[q], s[q]), p1 = mx4_bf16<b>(c[q + 1], s[q + 1]);
+                    lo[q / 2] = __builtin_amdgcn_perm(p1, p0, 0x05040100u);
+                    hi[q / 2] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
+                }
+                acc[2 * b] = RowMfma<bf16_t>::step(lo, yv[0], acc[2 * b], 0);
+                acc[2 * b + 1] = RowMfma<bf16_t>::step(hi, yv[0], acc[2 * b + 1], 0);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const f32x2_t p = mx4_f32<b>(c[q], s[q]);
+                    const float v = __uint_as_float(yv[q / 4][q % 4]);
+                    acc[2 * b] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[0], v, acc[2 * b], 0, 0, 0);
+                    acc[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[1], v, acc[2 * b + 1], 0, 0, 0);
+                }
+            }
+        };
+        columns(std::integral_constant<int, 0>{});
+        columns(std::integral_constant<int, 1>{});
+        columns(std::integral_constant<int, 2>{});
+        columns(std::integral_constant<int, 3>{});
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) red[wave][i][lane] = acc[i];
+    __syncthreads();
+    // thread (row, column octet): octet 4 g + v of the row's 128 columns
+    const int row = threadIdx.x >> 4, octet = threadIdx.x & 15;
+    const int ko = kb + octet * 8;
+    if (row0 + row >= row_end || ko >= K) return;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int from = (octet >> 2) * 16 + row;
+        v[i] = red[0][i][from][octet & 3];
+#pragma unroll
+        for (int w = 1; w < KS; ++w) v[i] += red[w][i][from][octet & 3];
+    }
+    const size_t at = static_cast<size_t>(row0 + row) * K + ko;
+    if (SLOPE) {
+        float uf[8];
+#pragma unroll
+        for (int i = 0; i < YV; ++i) Store<T>::unpack(*reinterpret_cast<const u32x4_t*>(u + at + i * Store<T>::kVec), uf + i * Store<T>::kVec);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= gelu_slope<T>(uf[i]);
+    }
+    store4(out + at, v);
+    store4(out + at + 4, v + 4);
+}
+
+namespace {
+
+// most row tiles of BM rows that a table of n segments with max_rows rows can have (one at least: a block reports the row count)
+long long tile_bound(const Segments& seg, int BM)
+{
+    const long long most = static_cast<long long>(seg.max_rows) / BM + seg.n;       // every segment may end in a part of a tile
+    const long long tiles = most < seg.max_rows ? most : seg.max_rows;              // ... and a tile has a row at least
+    return tiles > 1 ? tiles : 1;
+}
+
+template <typename T, bool GELU>
+void rows_product(const void* x, const int32_t* row_index, int row_div, const Segments& seg, int N, int K, const Mx4& W, const float* bias,
+                  void* pre, void* out, const int32_t* out_index, int32_t* status, hipStream_t stream)
+{
+    constexpr int NT = 2, KS = 4;
+    const long long blocks = tile_bound(seg, 16) * ((N + 16 * NT - 1) / (16 * NT));
+    hipLaunchKernelGGL((mx4_rows_kernel<T, NT, KS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream, static_cast<const T*>(x),
+                       row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index, status);
+}
+
+template <typename T, bool SLOPE>
+void transposed_product(const void* y, const Segments& seg, int N, int K, const Mx4& W, const void* u, void* out, int32_t* status, hipStream_t stream)
+{
+    const long long blocks = tile_bound(seg, 16) * ((K + 127) / 128);
+    hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, static_cast<const T*>(y), seg, N,
+                       K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
+}
+
+template <typename T>
+hipError_t ffn_t(const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F, const Mx4& W1, const float* b1,
+                 const Mx4& W2, const float* b2, void* pre, void* h_out, const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream)
+{
+    rows_product<T, true>(x_rows, row_index, row_div, seg, F, d, W1, b1, pre, hidden, nullptr, status, stream);
+    if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+    rows_product<T, false>(hidden, nullptr, 1, seg, d, F, W2, b2, nullptr, h_out, out_index, nullptr, stream);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t ffn_backward_t(const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1, const Mx4& W2, void* du, void* dx,
+                          int32_t* status, hipStream_t stream)
+{
+    transposed_product<T, true>(dh, seg, d, F, W2, u, du, status, stream);
+    if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+    transposed_product<T, false>(du, seg, F, d, W1, nullptr, dx, nullptr, stream);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
+                                 const Mx4& W1, const float* b1, const Mx4& W2, const float* b2, void* pre, void* h_out,
+                                 const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream)
+{
+    return (bf16 ? ffn_t<bf16_t> : ffn_t<float>)(x_rows, row_index, row_div, seg, d, F, W1, b1, W2, b2, pre, h_out, out_index, hidden, status, stream);
+}
+
+hipError_t launch_expert_ffn_mx4_backward(bool bf16, const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1,
+                                          const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream)
+{
+    return (bf16 ? ffn_backward_t<bf16_t> : ffn_backward_t<float>)(dh, u, seg, d, F, W1, W2, du, dx, status, stream);
+}
+
+}  // namespace dicemoe
