@@ -7,63 +7,9 @@
 #include "ffn_mfma.hpp"
 #include "kernels.hpp"
 #include "mx4.hpp"
+#include "mx4_tile.hpp"
 
 namespace dicemoe {
-
-// Phi(-a) for a in 0 .. 6: the polynomial that gelu_erf_fast has in its body
-__device__ __forceinline__ float normal_tail(float a) {
-    float p = fmaf(0x1.159ab2p-15f, a, -0x1.934b26p-11f);
-    p = fmaf(p, a, 0x1.08ca02p-7f);
-    p = fmaf(p, a, -0x1.b58d52p-5f);
-    p = fmaf(p, a, -0x1.d5c80ep-2f);
-    p = fmaf(p, a, -0x1.26b528p+0f);
-    p = fmaf(p, a, -0x1.ffff18p-1f);
-    return __builtin_amdgcn_exp2f(p);
-}
-// gelu and its slope.  The bf16 forms use that polynomial; NaN stays NaN in all of them.
-template <typename T> __device__ __forceinline__ float mx4_gelu(float u);
-template <> __device__ __forceinline__ float mx4_gelu<float>(float u) { return gelu_erf(u); }
-template <> __device__ __forceinline__ float mx4_gelu<bf16_t>(float u) { return u != u ? u : gelu_erf_fast(u); }
-// gelu'(u) = Phi(u) + u phi(u); with a = |u| it is 1 - s for u >= 0 and s below, s = Phi(-a) - a phi(a)
-template <typename T> __device__ __forceinline__ float gelu_slope(float u);
-template <> __device__ __forceinline__ float gelu_slope<float>(float u) {
-    return 0.5f * (1.0f + erff(u * 0.70710678118654752440f)) + u * (0.39894228040143267794f * expf(-0.5f * u * u));
-}
-template <> __device__ __forceinline__ float gelu_slope<bf16_t>(float u) {
-    const float a = fminf(fabsf(u), 6.0f);
-    const float bell = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * a * a);
-    const float s = normal_tail(a) - a * bell;
-    return u != u ? u : (u >= 0.0f ? 1.0f - s : s);
-}
-
-// The segment that row tile `tile` (BM rows, tiles of a segment contiguous) belongs to, found 64 segments at a time by lanes; all lanes
-// of a wavefront get the same answer.  Rows from max_rows on and segments of no known expert have no tiles.
-__device__ __forceinline__ bool find_tile(const Segments& s, int BM, int tile, int& expert, int& row0, int& row_end)
-{
-    const int lane = lane_id();
-    for (int base = 0; base < s.n; base += kWave) {
-        int begin = 0, end = 0, e = -1;
-        if (base + lane < s.n) {
-            begin = s.offsets[base + lane];
-            end = s.offsets[base + lane + 1];
-            e = s.expert[base + lane];
-            end = end < s.max_rows ? end : s.max_rows;
-        }
-        const bool used = end > begin && begin >= 0 && e >= 0 && e < s.n_experts;
-        const int upto = wave_scan(used ? (end - begin + BM - 1) / BM : 0);     // tiles of the lanes up to this one
-        const uint64_t past = __ballot(upto > tile);
-        if (past != 0) {
-            const int src = __ffsll(static_cast<unsigned long long>(past)) - 1;
-            const int before = src > 0 ? __builtin_amdgcn_readlane(upto, src - 1) : 0;
-            expert = __builtin_amdgcn_readlane(e, src);
-            row0 = __builtin_amdgcn_readlane(begin, src) + (tile - before) * BM;
-            row_end = __builtin_amdgcn_readlane(end, src);
-            return true;
-        }
-        tile -= __builtin_amdgcn_readlane(upto, kWave - 1);
-    }
-    return false;
-}
 
 __device__ __forceinline__ void store4(bf16_t* p, const float* v) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -262,6 +208,15 @@ template <typename T, bool GELU>
 void rows_product(const void* x, const int32_t* row_index, int row_div, const Segments& seg, int N, int K, const Mx4& W, const float* bias,
                   void* pre, void* out, const int32_t* out_index, int32_t* status, hipStream_t stream)
 {
+    if constexpr (sizeof(T) == 2) {
+        if (seg.max_rows >= 32 * seg.n) {
+            constexpr int NT = 4, RT = 2, WN = 2, WR = 2;
+            const long long blocks = tile_bound(seg, 32 * RT * WR) * ((N + 32 * NT * WN - 1) / (32 * NT * WN));
+            hipLaunchKernelGGL((mx4_tile_kernel<NT, RT, WN, WR, GELU>), dim3(static_cast<unsigned>((blocks + 7) / 8 * 8)), dim3(64 * WN * WR), 0, stream,
+                               static_cast<const T*>(x), row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index, status);
+            return;
+        }
+    }
     constexpr int NT = 2, KS = 4;
     const long long blocks = tile_bound(seg, 16) * ((N + 16 * NT - 1) / (16 * NT));
     hipLaunchKernelGGL((mx4_rows_kernel<T, NT, KS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream, static_cast<const T*>(x),
