@@ -12,6 +12,7 @@ struct moe_ctx {
     moe_shape shape;
     char err[256];
     uint64_t ffn_ready;     // bit v: the FFN kernels' per-device attributes have been set on device v
+    uint64_t mx4_ready;     // ... those of the 4-bit FFN kernels
     hipEvent_t ffn_between; // profiling aid: recorded between the two GEMMs of every expert FFN call (or null)
 };
 
@@ -237,6 +238,7 @@ int moe_create(moe_ctx** out, const moe_shape* s)
     ctx->shape.renorm_topk = s->renorm_topk ? 1 : 0;
     ctx->err[0] = '\0';
     ctx->ffn_ready = 0;
+    ctx->mx4_ready = 0;
     ctx->ffn_between = nullptr;
     *out = ctx;
     return MOE_OK;
@@ -347,6 +349,18 @@ int moe_dispatch_noalloc(moe_ctx* ctx, const void* x, const int32_t* expert_idx,
 
 }  // extern "C"
 
+// per-device kernel attributes, once per context and device (a context serves one host thread at a time)
+static int once_per_device(moe_ctx* ctx, const char* who, uint64_t* ready, hipError_t (*prepare)())
+{
+    int device = 0;
+    if (hipError_t err = hipGetDevice(&device); err != hipSuccess) return hip_result(ctx, err, who);
+    const bool tracked = device >= 0 && device < 64;
+    if (tracked && ((*ready >> device) & 1u)) return MOE_OK;
+    if (hipError_t err = prepare(); err != hipSuccess) return hip_result(ctx, err, who);
+    if (tracked) *ready |= 1ull << device;
+    return MOE_OK;
+}
+
 static int expert_ffn_common(moe_ctx* ctx, const char* who, const void* x_rows, const int32_t* row_pairs,
                              const int32_t* seg_offsets, const int32_t* seg_expert, int32_t n_segments,
                              int32_t max_rows, const void* W1, const float* b1, const void* W2, const float* b2,
@@ -355,14 +369,7 @@ static int expert_ffn_common(moe_ctx* ctx, const char* who, const void* x_rows, 
 {
     const moe_shape& s = ctx->shape;
     if (int rc = check_ffn(ctx, who, x_rows, seg_offsets, seg_expert, n_segments, max_rows, W1, W2, h_packed, workspace)) return rc;
-    // per-device kernel attributes, once per context and device (a context serves one host thread at a time)
-    int device = 0;
-    if (hipError_t err = hipGetDevice(&device); err != hipSuccess) return hip_result(ctx, err, who);
-    const bool tracked = device >= 0 && device < 64;
-    if (!tracked || !((ctx->ffn_ready >> device) & 1u)) {
-        if (hipError_t err = dicemoe::prepare_expert_ffn(); err != hipSuccess) return hip_result(ctx, err, who);
-        if (tracked) ctx->ffn_ready |= 1ull << device;
-    }
+    if (int rc = once_per_device(ctx, who, &ctx->ffn_ready, dicemoe::prepare_expert_ffn)) return rc;
     char* ws = static_cast<char*>(workspace);
     return hip_result(ctx,
                       launch_expert_ffn(is_bf16(ctx), x_rows, row_pairs, slots(ctx), seg_offsets, seg_expert, n_segments,
@@ -571,6 +578,7 @@ int moe_expert_ffn_mx4(moe_ctx* ctx, const void* x_rows, const int32_t* row_pair
     if (max_rows == 0) x_rows = h_rows = workspace;      // no row is read or written: an empty tensor's null will do
     if (int rc = check_ffn(ctx, who, x_rows, seg_offsets, seg_expert, n_segments, max_rows, W1_codes, W2_codes, h_rows, workspace)) return rc;
     if (!W1_scales || !W2_scales) return fail(ctx, MOE_ERR_NULL, "moe_expert_ffn_mx4: scales are null");
+    if (int rc = once_per_device(ctx, who, &ctx->mx4_ready, dicemoe::prepare_expert_ffn_mx4)) return rc;
     const moe_shape& s = ctx->shape;
     const Segments seg = {seg_offsets, seg_expert, n_segments, experts(ctx), max_rows};
     int32_t* const status = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + status_offset(ctx));
@@ -591,6 +599,7 @@ int moe_expert_ffn_mx4_backward(moe_ctx* ctx, const void* dh_packed, const void*
     if (max_rows == 0) dh_packed = u_packed = dx_packed = workspace;
     if (int rc = check_ffn(ctx, who, dh_packed, seg_offsets, seg_expert, n_segments, max_rows, W1_codes, W2_codes, dx_packed, workspace)) return rc;
     if (!u_packed || !W1_scales || !W2_scales) return fail(ctx, MOE_ERR_NULL, "moe_expert_ffn_mx4_backward: null pointer");
+    if (int rc = once_per_device(ctx, who, &ctx->mx4_ready, dicemoe::prepare_expert_ffn_mx4)) return rc;
     const moe_shape& s = ctx->shape;
     const Segments seg = {seg_offsets, seg_expert, n_segments, experts(ctx), max_rows};
     int32_t* const status = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + status_offset(ctx));

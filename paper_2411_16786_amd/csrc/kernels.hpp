@@ -105,6 +105,8 @@ struct Segments { const int32_t* offsets; const int32_t* expert; int n, n_expert
 hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
                                  const Mx4& W1, const float* b1, const Mx4& W2, const float* b2, void* pre, void* h_out,
                                  const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream);
+// Once per device before the first of these launches there: raises the dynamic-LDS limit of the tiled kernels.
+hipError_t prepare_expert_ffn_mx4();
 // du = (dh W2) gelu'(u), dx = du W1, row by row of the packed order
 hipError_t launch_expert_ffn_mx4_backward(bool bf16, const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1,
                                           const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream);

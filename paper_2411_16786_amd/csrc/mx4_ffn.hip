@@ -204,16 +204,84 @@ long long tile_bound(const Segments& seg, int BM)
     return tiles > 1 ? tiles : 1;
 }
 
+// The tiles of mx4_tile_kernel by size: 32 RT rows x 32 WN columns
+template <int RT_, int WN_> struct Tile { static constexpr int RT = RT_, WN = WN_; };
+constexpr int kTiles = 4, kTileRows[kTiles] = {128, 128, 64, 32}, kTileColumns[kTiles] = {256, 128, 128, 128};
+
+// Scales by chunks where all of them at once would leave less than three workgroups per compute unit: 4608 -> 1152 with 256 x 128
+// tiles 103 us instead of 113 and with 128 x 128 92 instead of 103, but with 128 x 64, where they leave three, 104 instead of 93
+int tile_lds(int tile, int K, bool chunks)
+{
+    const int BN = kTileColumns[tile], unit = 32 * BN;           // (a workgroup's 16-byte loads)
+    return 2 * kTileRows[tile] * 128 + 2 * BN * 64 + (chunks ? 2 * BN * 16 : (BN / 32 * K + unit - 1) / unit * unit);
+}
+bool tile_chunks(int tile, int K) { return K % 512 == 0 && 3 * tile_lds(tile, K, false) > kLdsBytes; }
+
+// Calls f with the shape of a tile and whether its scales go by chunks
+template <typename F>
+void with_tile(int tile, int K, F&& f)
+{
+    const bool chunks = tile_chunks(tile, K);
+    auto go = [&](auto shape) {
+        if (chunks) f(shape, std::true_type{});
+        else f(shape, std::false_type{});
+    };
+    if (tile == 0) go(Tile<4, 8>{});
+    else if (tile == 1) go(Tile<4, 4>{});
+    else if (tile == 2) go(Tile<2, 4>{});
+    else go(Tile<1, 4>{});
+}
+
+// Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel).  Below 16 rows a segment a tile of 32 is mostly padding.  Among the
+// tiles that with their scales fit the LDS the cheapest by area: what the compute unit with the most tiles has to do, at the rates
+// measured where all are busy (1152 -> 4608 of 8192 rows 85, 91, 93 and 119 us without GELU).
+int pick_tile(const Segments& seg, int N, int K)
+{
+    if (seg.max_rows < 16 * seg.n) return -1;
+    constexpr float slow[kTiles] = {1.0f, 1.08f, 1.12f, 1.4f};
+    int best = -1;
+    float least = 0.f;
+    for (int i = 0; i < kTiles; ++i) {
+        if (tile_lds(i, K, tile_chunks(i, K)) > kLdsBytes) continue;
+        const long long row_tiles = (seg.max_rows + seg.n * kTileRows[i] / 2) / kTileRows[i];        // (a segment's last tile is half full on average)
+        const long long tiles = (row_tiles > seg.n ? row_tiles : seg.n) * ((N + kTileColumns[i] - 1) / kTileColumns[i]);
+        const float cost = slow[i] * static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (kTileRows[i] * kTileColumns[i]);
+        if (best < 0 || cost < least) { best = i; least = cost; }
+    }
+    return best;
+}
+
+template <int RT, int WN, bool CHUNKS, bool GELU>
+hipError_t configure_tile()
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tile_kernel<RT, WN, CHUNKS, GELU>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+}
+template <int RT, int WN>
+hipError_t configure_tiles()
+{
+    hipError_t err = configure_tile<RT, WN, false, false>();
+    if (err == hipSuccess) err = configure_tile<RT, WN, false, true>();
+    if (err == hipSuccess) err = configure_tile<RT, WN, true, false>();
+    if (err == hipSuccess) err = configure_tile<RT, WN, true, true>();
+    return err;
+}
+
 template <typename T, bool GELU>
 void rows_product(const void* x, const int32_t* row_index, int row_div, const Segments& seg, int N, int K, const Mx4& W, const float* bias,
                   void* pre, void* out, const int32_t* out_index, int32_t* status, hipStream_t stream)
 {
     if constexpr (sizeof(T) == 2) {
-        if (seg.max_rows >= 32 * seg.n) {
-            constexpr int NT = 4, RT = 2, WN = 2, WR = 2;
-            const long long blocks = tile_bound(seg, 32 * RT * WR) * ((N + 32 * NT * WN - 1) / (32 * NT * WN));
-            hipLaunchKernelGGL((mx4_tile_kernel<NT, RT, WN, WR, GELU>), dim3(static_cast<unsigned>((blocks + 7) / 8 * 8)), dim3(64 * WN * WR), 0, stream,
-                               static_cast<const T*>(x), row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index, status);
+        const int tile = pick_tile(seg, N, K);
+        if (tile >= 0) {
+            with_tile(tile, K, [&](auto shape, auto chunks) {
+                constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN;
+                constexpr bool CHUNKS = decltype(chunks)::value;
+                typedef TileShape<RT, WN, CHUNKS> S;
+                const long long blocks = (tile_bound(seg, S::BR) * ((N + S::BN - 1) / S::BN) + 7) / 8 * 8;
+                hipLaunchKernelGGL((mx4_tile_kernel<RT, WN, CHUNKS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), S::lds_bytes(K), stream,
+                                   static_cast<const T*>(x), row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index,
+                                   status);
+            });
             return;
         }
     }
@@ -252,6 +320,15 @@ hipError_t ffn_backward_t(const void* dh, const void* u, const Segments& seg, in
 }
 
 }  // namespace
+
+hipError_t prepare_expert_ffn_mx4()
+{
+    hipError_t err = configure_tiles<4, 8>();
+    if (err == hipSuccess) err = configure_tiles<4, 4>();
+    if (err == hipSuccess) err = configure_tiles<2, 4>();
+    if (err == hipSuccess) err = configure_tiles<1, 4>();
+    return err;
+}
 
 hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
                                  const Mx4& W1, const float* b1, const Mx4& W2, const float* b2, void* pre, void* h_out,

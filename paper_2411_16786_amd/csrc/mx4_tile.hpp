@@ -1,14 +1,21 @@
 // Grouped product of many rows on 4-bit weights (bf16 rows), out[r, n] = act(sum_k x[r, k] W_e[n, k] + b_e[n]), tiled through LDS.
 //
-// A workgroup of WN x WR wavefronts owns BN = 32 NT WN columns n of BR = 32 RT WR rows; a wavefront NT x RT blocks of 32 x 32
-// (v_mfma_f32_32x32x16_bf16, weights first operand, rows second: a result register holds columns of one row).  The
-// reduction goes in stages of 64: rows take 128 bytes each, codes 32, so the weights cost a quarter of the LDS space and reads that a bf16
-// operand would, and one conversion instruction per two weights, in the shadow of the NT RT matrix instructions that it feeds.
-// A lane's 16 bytes of codes are one scale group: lane (h, c) = (l / 32, l % 32) holds k = 32 h .. + 31 of a stage for one weight row, instruction q
-// takes its q-th dword, and the rows' operand is read in the same order (16-byte chunk 4 h + q of the row).
-// Stages are double-buffered: the next stage's bytes are asked for into registers before this one's products and written to the
-// other buffer behind them, one barrier per stage; two workgroups per compute unit cover each other's barriers.
+// A workgroup of WN wavefronts owns 32 WN columns n of 32 RT rows; wavefront w the 32 columns from 32 w, all rows: RT blocks of 32 x 32
+// (v_mfma_f32_32x32x16_bf16, weights first operand, rows second: a result register holds columns of one row).  The reduction goes in
+// stages of 64: 128 bytes of a row, 32 of codes, so the weights take a quarter of the LDS space and reads of a bf16 operand and
+// are converted in one wavefront only, one instruction per two weights in the shadow of the RT matrix instructions that use them.
+// A lane's 16 bytes of codes are one scale group: lane (h, c) = (l / 32, l % 32) holds k = 32 h .. + 31 of a stage for one weight row, slice
+// q of the stage takes its q-th dword, and the rows' operand is read in the same order (16-byte chunk 4 h + q of the row).
+//
+// Direct-to-LDS loads, two stages of rows and two pairs of stages of codes in the LDS: what a stage has left is asked for again behind
+// its barrier, which stands before the stage's last slice, so that barrier and first reads of the next stage lie behind matrix
+// instructions.  What bounds it is the instruction stream between matrix instructions and the wait for the next stage; more wavefronts
+// per SIMD hide both, which is why the rings are short.  8192 rows over 8 experts (us; this library's bf16 GEMMs take 105 with GELU
+// and 92): 1152 -> 4608 with GELU, 256 x 128 tiles 91, 128 x 128 102, 128 x 64 100; 4608 -> 1152, 128 x 64 93, 128 x 128 92,
+// 256 x 128 103.  Rings of three stages, one workgroup less per compute unit: 113, 101, 105 and 103, 123, 115.  Stages through
+// registers: 110 and 122 at best.
 #pragma once
+#include <type_traits>
 #include "ffn_mfma.hpp"
 #include "kernels.hpp"
 #include "mx4.hpp"
@@ -70,6 +77,7 @@ __device__ __forceinline__ bool find_tile(const Segments& s, int BM, int tile, i
     return false;
 }
 
+__device__ __forceinline__ void wait_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(0xF | (0x3 << 14) | (0x7 << 4)); }
 __device__ __forceinline__ void store8(bf16_t* p, const float* v) {
     *reinterpret_cast<u32x4_t*>(p) = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
 }
@@ -103,134 +111,201 @@ __device__ __forceinline__ bool find_tile_on_xcd(const Segments& s, int BM, int 
     return find_tile(s, BM, tile, at.expert, at.row0, at.row_end);
 }
 
-template <int NT, int RT, int WN, int WR, bool GELU>
-__global__ __launch_bounds__(64 * WN * WR, 2) void mx4_tile_kernel(const bf16_t* __restrict__ x, const int32_t* __restrict__ row_index, int row_div,
-                                                                  Segments seg, int N, int K, Mx4 W, const float* __restrict__ bias,
-                                                                  bf16_t* __restrict__ pre, bf16_t* __restrict__ out,
-                                                                  const int32_t* __restrict__ out_index, int32_t* __restrict__ status)
+// BN columns, BR rows.  CHUNKS: scales in chunks of 512 reduction columns (16 bytes a row, two chunks in the LDS; K % 512 == 0) instead
+// of all of them at once (rows of weights are adjacent in memory, so is what is staged).
+constexpr int kLdsBytes = 160 * 1024;
+template <int RT, int WN, bool CHUNKS> struct TileShape {
+    static constexpr int BN = 32 * WN, BR = 32 * RT, kThreads = 64 * WN;
+    static constexpr int kRowBytes = BR * 128, kCodeBytes = BN * 64;           // of a stage, of a pair of stages
+    static constexpr int kRowLoads = kRowBytes / 16 / kThreads, kCodeLoads = kCodeBytes / 16 / kThreads;       // per wavefront
+    static_assert(kRowBytes % (16 * kThreads) == 0 && kCodeBytes % (16 * kThreads) == 0, "whole loads");
+    static constexpr int scale_bytes(int K) { return CHUNKS ? 2 * BN * 16 : (BN / 32 * K + 16 * kThreads - 1) / (16 * kThreads) * (16 * kThreads); }
+    static constexpr int lds_bytes(int K) { return 2 * kRowBytes + 2 * kCodeBytes + scale_bytes(K); }
+};
+
+template <int RT, int WN, bool CHUNKS, bool GELU>
+__global__ __launch_bounds__(64 * WN, 2) void mx4_tile_kernel(const bf16_t* __restrict__ x, const int32_t* __restrict__ row_index, int row_div,
+                                                           Segments seg, int N, int K, Mx4 W, const float* __restrict__ bias,
+                                                           bf16_t* __restrict__ pre, bf16_t* __restrict__ out,
+                                                           const int32_t* __restrict__ out_index, int32_t* __restrict__ status)
 {
-    constexpr int BN = 32 * NT * WN, BR = 32 * RT * WR, THREADS = 64 * WN * WR;
-    constexpr int XC = BR * 8 / THREADS, CC = (BN * 2 + THREADS - 1) / THREADS;      // 16-byte chunks per thread and stage
-    __shared__ u32x4_t xs[2][BR * 8];
-    __shared__ u32x4_t cs[2][BN * 2];
+    typedef TileShape<RT, WN, CHUNKS> S;
+    constexpr int BN = S::BN, BR = S::BR, XC = S::kRowLoads, CC = S::kCodeLoads;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    char* const code_lds = lds + 2 * S::kRowBytes;
+    char* const scale_lds = code_lds + 2 * S::kCodeBytes;
     report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
     const int n_blocks = (N + BN - 1) / BN;
     TilePlace at;
     if (!find_tile_on_xcd(seg, BR, n_blocks, blockIdx.x, at)) return;
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int wn = wave % WN, wr = wave / WN;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     const int half = lane >> 5, c32 = lane & 31;
     const int nb = at.block * BN;
 
-    // what this thread stages: chunk c of rows is (row c / 8, place c % 8), the place holding source chunk place ^ (row / 2 % 8), and
-    // chunk c of codes (row c / 2, place c % 2) with source chunk place ^ (row / 16 % 2): reads of 32 rows then spread over all banks
-    const bf16_t* xp[XC];
-    const uint8_t* cp[CC];
+    // Rows in the LDS: 16-byte chunk c of a row's 128 bytes lies at place c ^ (row / 2 % 8).  Codes: chunk c of a row's 64 bytes at
+    // place c ^ (bits 2 and 4 of the row).  Reads of 16 rows at a time then touch every bank once.
+    uint32_t x_from[XC], c_from[CC], c_second[CC];              // byte offsets from x and from the tile's first code; 32 for a chunk of an odd stage
 #pragma unroll
     for (int i = 0; i < XC; ++i) {
-        const int c = threadIdx.x + i * THREADS, row = c >> 3;
+        const int row = (wave * XC + i) * 8 + (lane >> 3);
         const int r = at.row0 + row < at.row_end ? at.row0 + row : at.row_end - 1;       // rows past the end repeat the last; never stored
-        xp[i] = x + static_cast<size_t>(row_index ? row_index[r] / row_div : r) * K + ((c & 7) ^ ((row >> 1) & 7)) * 8;
+        x_from[i] = static_cast<uint32_t>(row_index ? row_index[r] / row_div : r) * (2u * K) + ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     }
+    const int rows_here = N - nb < BN ? N - nb : BN;            // columns past N repeat the last; never stored
 #pragma unroll
     for (int i = 0; i < CC; ++i) {
-        const int c = threadIdx.x + i * THREADS, row = (c >> 1) & (BN - 1);
-        const int n = nb + row < N ? nb + row : N - 1;
-        cp[i] = W.codes + (static_cast<size_t>(at.expert) * N + n) * (K / 2) + ((c & 1) ^ ((row >> 4) & 1)) * 16;
+        const int row = (wave * CC + i) * 16 + (lane >> 2);
+        const uint32_t chunk = (lane & 3) ^ (((row >> 2) & 1) | ((row >> 3) & 2));
+        c_from[i] = static_cast<uint32_t>(row < rows_here ? row : rows_here - 1) * (K / 2) + chunk * 16;
+        c_second[i] = (chunk & 2) * 16;
     }
-    const uint8_t* sp[NT];
-    int c_off[NT], x_off[4];
-    const int wrow = tile_weight_row(c32);
+    const size_t first = static_cast<size_t>(at.expert) * N + nb;
+    const char* const x_base = reinterpret_cast<const char*>(x);
+    const char* const c_base = reinterpret_cast<const char*>(W.codes) + first * (K / 2);
+    const char* const s_base = reinterpret_cast<const char*>(W.scales) + first * (K / kMxGroup);
+    const int wrow = wave * 32 + tile_weight_row(c32);
+    const int c_off = wrow * 64 + ((half ^ (((wrow >> 2) & 1) | ((wrow >> 3) & 2))) * 16);      // of an even stage; an odd one's place has bit 1 flipped
+    const int s_off = CHUNKS ? wrow * 16 + half : wrow * (K / kMxGroup) + half;
+    int x_off[4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = (wn * NT + t) * 32 + wrow;
-        const int n = nb + row < N ? nb + row : N - 1;
-        sp[t] = W.scales + (static_cast<size_t>(at.expert) * N + n) * (K / kMxGroup) + half;
-        c_off[t] = row * 2 + (half ^ ((row >> 4) & 1));
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int row = wr * RT * 32 + c32;
-        x_off[q] = row * 8 + ((half * 4 + q) ^ ((row >> 1) & 7));
-    }
+    for (int q = 0; q < 4; ++q) x_off[q] = (c32 * 8 + ((half * 4 + q) ^ ((c32 >> 1) & 7))) * 16;
 
-    f32x16_v acc[NT][RT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[t][r][v] = 0.f;
-    const bool live = at.row0 + wr * RT * 32 < at.row_end && nb + wn * NT * 32 < N;
-
-    u32x4_t xv[XC], cv[CC];
-    uint32_t sv[NT];
-    auto ask = [&](int s) {
-#pragma unroll
-        for (int i = 0; i < CC; ++i) cv[i] = *reinterpret_cast<const u32x4_t*>(cp[i] + s * 32);
-#pragma unroll
-        for (int i = 0; i < XC; ++i) xv[i] = *reinterpret_cast<const u32x4_t*>(xp[i] + s * 64);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) sv[t] = sp[t][s * 2];
-    };
-    auto keep = [&](int b) {
-#pragma unroll
-        for (int i = 0; i < CC; ++i)
-            if (BN * 2 % THREADS == 0 || static_cast<int>(threadIdx.x) + i * THREADS < BN * 2) cs[b][threadIdx.x + i * THREADS] = cv[i];
-#pragma unroll
-        for (int i = 0; i < XC; ++i) xs[b][threadIdx.x + i * THREADS] = xv[i];
-    };
     const int stages = K / 64;
-    ask(0);
-    keep(0);
-    float scale[NT];
+    auto ask_rows = [&](int s, int place) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) scale[t] = mx4_scale(sv[t]);
-    __syncthreads();
-    for (int s = 0; s < stages; ++s) {
-        const int b = s & 1;
-        if (s + 1 < stages) ask(s + 1);
-        if (live) {
-            u32x4_t codes[NT];
+        for (int i = 0; i < XC; ++i) {
+            const char* from = x_base + static_cast<size_t>(s) * 128;
+            uint32_t off = x_from[i];
+            asm volatile("" : "+s"(from), "+v"(off));           // scalar base and 32-bit offset: no address arithmetic per lane
+            __builtin_amdgcn_global_load_lds(DICEMOE_GLOBAL_PTR(from + off), DICEMOE_LDS_PTR(lds + place * S::kRowBytes + (wave * XC + i) * 1024), 16, 0, 0);
+        }
+    };
+    auto ask_codes = [&](int pair) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) codes[t] = cs[b][c_off[t]];
+        for (int i = 0; i < CC; ++i) {
+            const char* from = c_base + static_cast<size_t>(pair) * 64;
+            uint32_t off = c_from[i];
+            if (2 * pair + 1 >= stages) off -= c_second[i];     // a last pair of one stage: the first half twice, the second is never read
+            asm volatile("" : "+s"(from), "+v"(off));
+            __builtin_amdgcn_global_load_lds(DICEMOE_GLOBAL_PTR(from + off), DICEMOE_LDS_PTR(code_lds + (pair & 1) * S::kCodeBytes + (wave * CC + i) * 1024), 16, 0, 0);
+        }
+    };
+    auto ask_scales = [&](int chunk) {                          // of stages 8 chunk .. + 7, 64 rows a wavefront
+        if (wave * 64 < BN) {
+            const int row = wave * 64 + lane;
+            const char* const from = s_base + static_cast<size_t>(row < rows_here ? row : rows_here - 1) * (K / kMxGroup) + chunk * 16;
+            __builtin_amdgcn_global_load_lds(DICEMOE_GLOBAL_PTR(from), DICEMOE_LDS_PTR(scale_lds + (chunk & 1) * BN * 16 + wave * 1024), 16, 0, 0);
+        }
+    };
+    // ahead of the first stage: scales, codes and rows of stage 0, rows of stage 1, codes of stages 2 and 3
+    if constexpr (CHUNKS) {
+        ask_scales(0);
+        if (stages > 8) ask_scales(1);
+    } else {
+        const int there = rows_here * (K / kMxGroup);
+        for (int to = wave * 1024; to < S::scale_bytes(K); to += S::kThreads * 16) {
+            const int mine = to + lane * 16;
+            __builtin_amdgcn_global_load_lds(DICEMOE_GLOBAL_PTR(s_base + (mine < there ? mine : 0)), DICEMOE_LDS_PTR(scale_lds + to), 16, 0, 0);
+        }
+    }
+    ask_codes(0);
+    ask_rows(0, 0);
+    if (stages > 1) ask_rows(1, 1);
+    if (stages > 2) ask_codes(1);
+    f32x16_v acc[RT];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                u32x4_t rows[RT];
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) rows[r] = xs[b][x_off[q] + r * 32 * 8];
+        for (int v = 0; v < 16; ++v) acc[r][v] = 0.f;
+    const bool live = nb + wave * 32 < N;
+
+    u32x4_t codes, rows[2][RT];
+    uint32_t byte = 0;
+    float scale = 0.f;
+    auto read_rows = [&](int set, int place, int q) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const u32x4_t a = {mx4_bf16<0>(codes[t][q], scale[t]), mx4_bf16<1>(codes[t][q], scale[t]),
-                                       mx4_bf16<2>(codes[t][q], scale[t]), mx4_bf16<3>(codes[t][q], scale[t])};
+        for (int r = 0; r < RT; ++r) rows[set][r] = *reinterpret_cast<const u32x4_t*>(lds + place * S::kRowBytes + x_off[q] + r * 4096);
+    };
+    auto read_weights = [&](int s, int odd) {
+        codes = *reinterpret_cast<const u32x4_t*>(code_lds + ((s >> 1) & 1) * S::kCodeBytes + (c_off ^ (odd * 32)));
+        byte = *reinterpret_cast<const uint8_t*>(scale_lds + s_off + (CHUNKS ? ((s >> 3) & 1) * BN * 16 + 2 * (s & 7) : 2 * s));
+    };
+    if (stages > 2) wait_vmcnt<XC + CC>();                      // (loads return in order: all but the last ones asked for have landed)
+    else wait_vmcnt<0>();
+    block_barrier();
+
+    auto stage = [&](int s, auto odd_tag, auto live_tag) {
+        constexpr int ODD = decltype(odd_tag)::value;
+        constexpr bool LIVE = decltype(live_tag)::value;
+        const bool more = s + 1 < stages;
 #pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        acc[t][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_v*>(&a),
-                                                                            *reinterpret_cast<const bf16x8_v*>(&rows[r]), acc[t][r], 0, 0, 0);
+        for (int q = 0; q < 4; ++q) {
+            u32x4_t a;
+            if (LIVE) a = u32x4_t{mx4_bf16<0>(codes[q], scale), mx4_bf16<1>(codes[q], scale), mx4_bf16<2>(codes[q], scale), mx4_bf16<3>(codes[q], scale)};
+            __builtin_amdgcn_sched_barrier(0);
+            if (q == 3 && more) {
+                wait_lgkmcnt0();                                // this wavefront has read all of stage s, whose place is filled next
+                // The rows of stage s + 1 and all that was asked for before them have landed once only the codes asked for behind them
+                // are under way: behind odd stages codes follow the rows (there are none behind the last rows)
+                if (ODD || s + 2 >= stages) wait_vmcnt<0>();
+                else wait_vmcnt<CC>();
+                block_barrier();
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (LIVE) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    acc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_v*>(&a), *reinterpret_cast<const bf16x8_v*>(&rows[q & 1][r]),
+                                                                     acc[r], 0, 0, 0);
+                    if (r == 0) {                               // what the next slice needs is read behind this one's first product
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (q < 3) {
+                            read_rows((q + 1) & 1, ODD, q + 1);
+                        } else if (more) {
+                            read_weights(s + 1, 1 - ODD);
+                            read_rows(0, 1 - ODD, 0);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (s + 1 < stages) {
-            keep(b ^ 1);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) scale[t] = mx4_scale(sv[t]);
+        if (s + 2 < stages) {
+            if (CHUNKS && ODD && (s & 7) == 7 && s + 9 < stages) ask_scales((s >> 3) + 2);
+            ask_rows(s + 2, ODD);
+            if (ODD && s + 3 < stages) ask_codes((s + 3) / 2);
         }
-        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        if (LIVE) scale = mx4_scale(byte);
+    };
+    auto run = [&](auto live_tag) {
+        if (decltype(live_tag)::value) {
+            read_weights(0, 0);
+            read_rows(0, 0, 0);
+            scale = mx4_scale(byte);
+        }
+        for (int s = 0; s < stages; s += 2) {
+            stage(s, std::integral_constant<int, 0>{}, live_tag);
+            if (s + 1 < stages) stage(s + 1, std::integral_constant<int, 1>{}, live_tag);
+        }
+    };
+    if (!live) {                                                // columns past N: its loads, waits and barriers only
+        run(std::false_type{});
+        return;
     }
-    if (!live) return;
+    run(std::true_type{});
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = at.row0 + (wr * RT + r) * 32 + c32;
+        const int row = at.row0 + r * 32 + c32;
         if (row >= at.row_end) continue;
         bf16_t* const to = out + static_cast<size_t>(out_index ? out_index[row] : row) * N;
         bf16_t* const pre_to = pre ? pre + static_cast<size_t>(row) * N : nullptr;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int n = nb + (wn * NT + t) * 32 + half * 16;
-            if (n >= N) continue;
+        {
+            const int n = nb + wave * 32 + half * 16;
             float v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[t][r][i];
+            for (int i = 0; i < 16; ++i) v[i] = acc[r][i];
             if (bias) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
