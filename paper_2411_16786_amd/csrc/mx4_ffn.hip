@@ -8,6 +8,7 @@
 #include "kernels.hpp"
 #include "mx4.hpp"
 #include "mx4_tile.hpp"
+#include "mx4_tile_t.hpp"
 
 namespace dicemoe {
 
@@ -232,6 +233,14 @@ void with_tile(int tile, int K, F&& f)
     else go(Tile<1, 4>{});
 }
 
+// What the compute unit with the most tiles of BM rows x BN columns has to do, by area
+float tile_cost(const Segments& seg, int BM, int BN, int columns)
+{
+    const long long row_tiles = (seg.max_rows + seg.n * BM / 2) / BM;                       // (a segment's last tile is half full on average)
+    const long long tiles = (row_tiles > seg.n ? row_tiles : seg.n) * ((columns + BN - 1) / BN);
+    return static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (BM * BN);
+}
+
 // Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel).  Below 16 rows a segment a tile of 32 is mostly padding.  Among the
 // tiles that with their scales fit the LDS the cheapest by area: what the compute unit with the most tiles has to do, at the rates
 // measured where all are busy (1152 -> 4608 of 8192 rows 85, 91, 93 and 119 us without GELU).
@@ -243,10 +252,31 @@ int pick_tile(const Segments& seg, int N, int K)
     float least = 0.f;
     for (int i = 0; i < kTiles; ++i) {
         if (tile_lds(i, K, tile_chunks(i, K)) > kLdsBytes) continue;
-        const long long row_tiles = (seg.max_rows + seg.n * kTileRows[i] / 2) / kTileRows[i];        // (a segment's last tile is half full on average)
-        const long long tiles = (row_tiles > seg.n ? row_tiles : seg.n) * ((N + kTileColumns[i] - 1) / kTileColumns[i]);
-        const float cost = slow[i] * static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (kTileRows[i] * kTileColumns[i]);
+        const float cost = slow[i] * tile_cost(seg, kTileRows[i], kTileColumns[i], N);
         if (best < 0 || cost < least) { best = i; least = cost; }
+    }
+    return best;
+}
+
+// The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns; the LDS does not depend on the reduction).  8192 rows, 4608 -> 1152:
+// 64 x 256 tiles 108 us, 64 x 128 124, 32 x 128 155, 128 x 256 131, 96 x 256 103; 2000 rows 75, 68, 65, 89, 81.
+constexpr int kTilesT = 3, kTileRowsT[kTilesT] = {64, 64, 32}, kTileColumnsT[kTilesT] = {256, 128, 128};
+template <typename F>
+void with_tile_t(int tile, F&& f)
+{
+    if (tile == 0) f(Tile<2, 4>{});
+    else if (tile == 1) f(Tile<2, 2>{});
+    else f(Tile<1, 2>{});
+}
+int pick_tile_t(const Segments& seg, int K)
+{
+    if (seg.max_rows < 16 * seg.n) return -1;
+    constexpr float slow[kTilesT] = {1.0f, 1.25f, 1.6f};
+    int best = 0;
+    float least = 0.f;
+    for (int i = 0; i < kTilesT; ++i) {
+        const float cost = slow[i] * tile_cost(seg, kTileRowsT[i], kTileColumnsT[i], K);
+        if (i == 0 || cost < least) { best = i; least = cost; }
     }
     return best;
 }
@@ -294,6 +324,19 @@ void rows_product(const void* x, const int32_t* row_index, int row_div, const Se
 template <typename T, bool SLOPE>
 void transposed_product(const void* y, const Segments& seg, int N, int K, const Mx4& W, const void* u, void* out, int32_t* status, hipStream_t stream)
 {
+    if constexpr (sizeof(T) == 2) {
+        const int tile = pick_tile_t(seg, K);
+        if (tile >= 0) {
+            with_tile_t(tile, [&](auto shape) {
+                constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN;
+                typedef TileShapeT<RT, WN> S;
+                const long long blocks = (tile_bound(seg, S::BR) * ((K + S::BK - 1) / S::BK) + 7) / 8 * 8;
+                hipLaunchKernelGGL((mx4_tile_transposed_kernel<RT, WN, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), S::kLds, stream,
+                                   static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
+            });
+            return;
+        }
+    }
     const long long blocks = tile_bound(seg, 16) * ((K + 127) / 128);
     hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, static_cast<const T*>(y), seg, N,
                        K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
@@ -327,7 +370,7 @@ hipError_t prepare_expert_ffn_mx4()
     if (err == hipSuccess) err = configure_tiles<4, 4>();
     if (err == hipSuccess) err = configure_tiles<2, 4>();
     if (err == hipSuccess) err = configure_tiles<1, 4>();
-    return err;
+    return err;                                                  // (the transposed tiles need less than the 64 KiB that every kernel has)
 }
 
 hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
