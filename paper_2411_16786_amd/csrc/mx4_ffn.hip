@@ -205,16 +205,19 @@ long long tile_bound(const Segments& seg, int BM)
     return tiles > 1 ? tiles : 1;
 }
 
-// The tiles of mx4_tile_kernel by size: 32 RT rows x 32 WN columns
-template <int RT_, int WN_> struct Tile { static constexpr int RT = RT_, WN = WN_; };
-constexpr int kTiles = 4, kTileRows[kTiles] = {128, 128, 64, 32}, kTileColumns[kTiles] = {256, 128, 128, 128};
+// The tiles of mx4_tile_kernel: 32 RT rows x 32 WN columns, the reduction in KS shares
+template <int RT_, int WN_, int KS_> struct Tile { static constexpr int RT = RT_, WN = WN_, KS = KS_; };
+struct TileSize { int rows, columns, shares; };
+constexpr int kTiles = 5, kFewTile = 3;
+constexpr TileSize kTile[kTiles] = {{128, 256, 1}, {128, 128, 1}, {64, 128, 1}, {32, 128, 2}, {32, 64, 4}};
 
 // Scales by chunks where all of them at once would leave less than three workgroups per compute unit: 4608 -> 1152 with 256 x 128
 // tiles 103 us instead of 113 and with 128 x 128 92 instead of 103, but with 128 x 64, where they leave three, 104 instead of 93
 int tile_lds(int tile, int K, bool chunks)
 {
-    const int BN = kTileColumns[tile], unit = 32 * BN;           // (a workgroup's 16-byte loads)
-    return 2 * kTileRows[tile] * 128 + 2 * BN * 64 + (chunks ? 2 * BN * 16 : (BN / 32 * K + unit - 1) / unit * unit);
+    const TileSize t = kTile[tile];
+    const int unit = 32 * t.columns * t.shares;                  // a workgroup's 16-byte loads
+    return t.shares * (2 * t.rows * 128 + 2 * t.columns * 64 + (chunks ? 2 * t.columns * 16 : 0)) + (chunks ? 0 : (t.columns / 32 * K + unit - 1) / unit * unit);
 }
 bool tile_chunks(int tile, int K) { return K % 512 == 0 && 3 * tile_lds(tile, K, false) > kLdsBytes; }
 
@@ -227,34 +230,48 @@ void with_tile(int tile, int K, F&& f)
         if (chunks) f(shape, std::true_type{});
         else f(shape, std::false_type{});
     };
-    if (tile == 0) go(Tile<4, 8>{});
-    else if (tile == 1) go(Tile<4, 4>{});
-    else if (tile == 2) go(Tile<2, 4>{});
-    else go(Tile<1, 4>{});
+    if (tile == 0) go(Tile<4, 8, 1>{});
+    else if (tile == 1) go(Tile<4, 4, 1>{});
+    else if (tile == 2) go(Tile<2, 4, 1>{});
+    else if (tile == 3) go(Tile<1, 4, 2>{});
+    else go(Tile<1, 2, 4>{});
 }
 
-// What the compute unit with the most tiles of BM rows x BN columns has to do, by area
-float tile_cost(const Segments& seg, int BM, int BN, int columns)
+// Tiles of BM rows x BN columns, a segment's last row tile half full on average
+long long tile_count(const Segments& seg, int BM, int BN, int columns)
 {
-    const long long row_tiles = (seg.max_rows + seg.n * BM / 2) / BM;                       // (a segment's last tile is half full on average)
-    const long long tiles = (row_tiles > seg.n ? row_tiles : seg.n) * ((columns + BN - 1) / BN);
-    return static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (BM * BN);
+    const long long row_tiles = (seg.max_rows + seg.n * BM / 2) / BM;
+    return (row_tiles > seg.n ? row_tiles : seg.n) * ((columns + BN - 1) / BN);
 }
+// ... and by area what the compute unit with the most of them has to do
+float tile_cost(long long tiles, int BM, int BN) { return static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (BM * BN); }
 
-// Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel).  Below 16 rows a segment a tile of 32 is mostly padding.  Among the
-// tiles that with their scales fit the LDS the cheapest by area: what the compute unit with the most tiles has to do, at the rates
-// measured where all are busy (1152 -> 4608 of 8192 rows 85, 91, 93 and 119 us without GELU).
+// Columns per wavefront set of mx4_rows_kernel: 16 while that gives each compute unit no more than six workgroups (4608 -> 1152, one token
+// 6.6 us against 9.6 with 32, eight tokens 9.1 and 10.0), else 32 (1152 -> 4608, eight tokens 9.2 against 11.6)
+bool rows_narrow(const Segments& seg, int N) { return tile_bound(seg, 16) * (N / 16) <= 6 * kComputeUnits; }
+
+// Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel), which up to four rows a segment is faster while it has at
+// most 12 workgroups per compute unit (eight tokens at the DiT-MoE-XL widths 9.2 and 9.1 us against 11.5 and 13.0; 26 rows over 16
+// experts, 2048 -> 8192, 27.8 against 22.6).  Among the tiles that with their scales fit the LDS the cheapest by area, at the
+// rates of 8192 -> 4096 of 8192 rows (444, 481 and 563 us; the tiles of 32 rows are for few rows); a compute unit with a single workgroup
+// of four wavefronts waits more.  Of the two of 32 rows, in shares, the narrower one in more shares while each tile has a compute unit
+// to itself (200 rows over 8 experts: 4608 -> 1152 13.4 us against 21.8, 1152 -> 4608, 288 tiles, 16.6 against 12.6).
 int pick_tile(const Segments& seg, int N, int K)
 {
-    if (seg.max_rows < 16 * seg.n) return -1;
-    constexpr float slow[kTiles] = {1.0f, 1.08f, 1.12f, 1.4f};
+    if (seg.max_rows <= 4 * seg.n && tile_bound(seg, 16) * (N / 32) <= 12 * kComputeUnits) return -1;
+    constexpr float slow[kTiles] = {1.0f, 1.08f, 1.27f, 2.5f};
     int best = -1;
     float least = 0.f;
-    for (int i = 0; i < kTiles; ++i) {
+    for (int i = 0; i <= kFewTile; ++i) {
         if (tile_lds(i, K, tile_chunks(i, K)) > kLdsBytes) continue;
-        const float cost = slow[i] * tile_cost(seg, kTileRows[i], kTileColumns[i], N);
+        const long long tiles = tile_count(seg, kTile[i].rows, kTile[i].columns, N);
+        float cost = slow[i] * tile_cost(tiles, kTile[i].rows, kTile[i].columns);
+        if (tiles <= kComputeUnits && kTile[i].columns * kTile[i].shares == 128) cost *= 1.3f;
         if (best < 0 || cost < least) { best = i; least = cost; }
     }
+    if (best == kFewTile && tile_count(seg, kTile[best].rows, kTile[best].columns, N) <= kComputeUnits &&
+        tile_lds(kFewTile + 1, K, tile_chunks(kFewTile + 1, K)) <= kLdsBytes)
+        ++best;
     return best;
 }
 
@@ -264,9 +281,9 @@ constexpr int kTilesT = 3, kTileRowsT[kTilesT] = {64, 64, 32}, kTileColumnsT[kTi
 template <typename F>
 void with_tile_t(int tile, F&& f)
 {
-    if (tile == 0) f(Tile<2, 4>{});
-    else if (tile == 1) f(Tile<2, 2>{});
-    else f(Tile<1, 2>{});
+    if (tile == 0) f(Tile<2, 4, 1>{});
+    else if (tile == 1) f(Tile<2, 2, 1>{});
+    else f(Tile<1, 2, 1>{});
 }
 int pick_tile_t(const Segments& seg, int K)
 {
@@ -275,25 +292,22 @@ int pick_tile_t(const Segments& seg, int K)
     int best = 0;
     float least = 0.f;
     for (int i = 0; i < kTilesT; ++i) {
-        const float cost = slow[i] * tile_cost(seg, kTileRowsT[i], kTileColumnsT[i], K);
+        const float cost = slow[i] * tile_cost(tile_count(seg, kTileRowsT[i], kTileColumnsT[i], K), kTileRowsT[i], kTileColumnsT[i]);
         if (i == 0 || cost < least) { best = i; least = cost; }
     }
     return best;
 }
 
-template <int RT, int WN, bool CHUNKS, bool GELU>
+template <typename Shape>
 hipError_t configure_tile()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tile_kernel<RT, WN, CHUNKS, GELU>), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-}
-template <int RT, int WN>
-hipError_t configure_tiles()
-{
-    hipError_t err = configure_tile<RT, WN, false, false>();
-    if (err == hipSuccess) err = configure_tile<RT, WN, false, true>();
-    if (err == hipSuccess) err = configure_tile<RT, WN, true, false>();
-    if (err == hipSuccess) err = configure_tile<RT, WN, true, true>();
-    return err;
+    const void* const kernels[] = {reinterpret_cast<const void*>(&mx4_tile_kernel<Shape::RT, Shape::WN, Shape::KS, false, false>),
+                                   reinterpret_cast<const void*>(&mx4_tile_kernel<Shape::RT, Shape::WN, Shape::KS, false, true>),
+                                   reinterpret_cast<const void*>(&mx4_tile_kernel<Shape::RT, Shape::WN, Shape::KS, true, false>),
+                                   reinterpret_cast<const void*>(&mx4_tile_kernel<Shape::RT, Shape::WN, Shape::KS, true, true>)};
+    for (const void* kernel : kernels)
+        if (hipError_t err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes); err != hipSuccess) return err;
+    return hipSuccess;
 }
 
 template <typename T, bool GELU>
@@ -304,21 +318,25 @@ void rows_product(const void* x, const int32_t* row_index, int row_div, const Se
         const int tile = pick_tile(seg, N, K);
         if (tile >= 0) {
             with_tile(tile, K, [&](auto shape, auto chunks) {
-                constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN;
+                constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN, KS = decltype(shape)::KS;
                 constexpr bool CHUNKS = decltype(chunks)::value;
-                typedef TileShape<RT, WN, CHUNKS> S;
+                typedef TileShape<RT, WN, KS, CHUNKS> S;
                 const long long blocks = (tile_bound(seg, S::BR) * ((N + S::BN - 1) / S::BN) + 7) / 8 * 8;
-                hipLaunchKernelGGL((mx4_tile_kernel<RT, WN, CHUNKS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), S::lds_bytes(K), stream,
-                                   static_cast<const T*>(x), row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index,
-                                   status);
+                hipLaunchKernelGGL((mx4_tile_kernel<RT, WN, KS, CHUNKS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * S::kThreads), S::lds_bytes(K),
+                                   stream, static_cast<const T*>(x), row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out),
+                                   out_index, status);
             });
             return;
         }
     }
-    constexpr int NT = 2, KS = 4;
-    const long long blocks = tile_bound(seg, 16) * ((N + 16 * NT - 1) / (16 * NT));
-    hipLaunchKernelGGL((mx4_rows_kernel<T, NT, KS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream, static_cast<const T*>(x),
-                       row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index, status);
+    auto go = [&](auto narrow) {
+        constexpr int NT = decltype(narrow)::value ? 1 : 2, KS = 8;
+        const long long blocks = tile_bound(seg, 16) * ((N + 16 * NT - 1) / (16 * NT));
+        hipLaunchKernelGGL((mx4_rows_kernel<T, NT, KS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream, static_cast<const T*>(x),
+                           row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index, status);
+    };
+    if (rows_narrow(seg, N)) go(std::true_type{});
+    else go(std::false_type{});
 }
 
 template <typename T, bool SLOPE>
@@ -366,10 +384,11 @@ hipError_t ffn_backward_t(const void* dh, const void* u, const Segments& seg, in
 
 hipError_t prepare_expert_ffn_mx4()
 {
-    hipError_t err = configure_tiles<4, 8>();
-    if (err == hipSuccess) err = configure_tiles<4, 4>();
-    if (err == hipSuccess) err = configure_tiles<2, 4>();
-    if (err == hipSuccess) err = configure_tiles<1, 4>();
+    hipError_t err = configure_tile<Tile<4, 8, 1>>();
+    if (err == hipSuccess) err = configure_tile<Tile<4, 4, 1>>();
+    if (err == hipSuccess) err = configure_tile<Tile<2, 4, 1>>();
+    if (err == hipSuccess) err = configure_tile<Tile<1, 4, 2>>();
+    if (err == hipSuccess) err = configure_tile<Tile<1, 2, 4>>();
     return err;                                                  // (the transposed tiles need less than the 64 KiB that every kernel has)
 }
 

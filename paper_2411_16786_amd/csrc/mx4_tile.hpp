@@ -114,33 +114,37 @@ __device__ __forceinline__ bool find_tile_on_xcd(const Segments& s, int BM, int 
 // BN columns, BR rows.  CHUNKS: scales in chunks of 512 reduction columns (16 bytes a row, two chunks in the LDS; K % 512 == 0) instead
 // of all of them at once (rows of weights are adjacent in memory, so is what is staged).
 constexpr int kLdsBytes = 160 * 1024;
-template <int RT, int WN, bool CHUNKS> struct TileShape {
-    static constexpr int BN = 32 * WN, BR = 32 * RT, kThreads = 64 * WN;
+template <int RT, int WN, int KS, bool CHUNKS> struct TileShape {
+    static constexpr int BN = 32 * WN, BR = 32 * RT, kThreads = 64 * WN;            // (of one share)
     static constexpr int kRowBytes = BR * 128, kCodeBytes = BN * 64;           // of a stage, of a pair of stages
     static constexpr int kRowLoads = kRowBytes / 16 / kThreads, kCodeLoads = kCodeBytes / 16 / kThreads;       // per wavefront
     static_assert(kRowBytes % (16 * kThreads) == 0 && kCodeBytes % (16 * kThreads) == 0, "whole loads");
-    static constexpr int scale_bytes(int K) { return CHUNKS ? 2 * BN * 16 : (BN / 32 * K + 16 * kThreads - 1) / (16 * kThreads) * (16 * kThreads); }
-    static constexpr int lds_bytes(int K) { return 2 * kRowBytes + 2 * kCodeBytes + scale_bytes(K); }
+    static constexpr int kShareBytes = 2 * kRowBytes + 2 * kCodeBytes + (CHUNKS ? 2 * BN * 16 : 0);
+    static constexpr int scale_bytes(int K) { return CHUNKS ? 0 : (BN / 32 * K + 16 * KS * kThreads - 1) / (16 * KS * kThreads) * (16 * KS * kThreads); }
+    static constexpr int lds_bytes(int K) { return KS * kShareBytes + scale_bytes(K); }
+    static_assert((KS - 1) * RT * 64 * kThreads <= KS * kShareBytes, "the shares' sums fit where their stages were");
 };
 
-template <int RT, int WN, bool CHUNKS, bool GELU>
-__global__ __launch_bounds__(64 * WN, 2) void mx4_tile_kernel(const bf16_t* __restrict__ x, const int32_t* __restrict__ row_index, int row_div,
+template <int RT, int WN, int KS, bool CHUNKS, bool GELU>
+__global__ __launch_bounds__(64 * WN * KS, 2) void mx4_tile_kernel(const bf16_t* __restrict__ x, const int32_t* __restrict__ row_index, int row_div,
                                                            Segments seg, int N, int K, Mx4 W, const float* __restrict__ bias,
                                                            bf16_t* __restrict__ pre, bf16_t* __restrict__ out,
                                                            const int32_t* __restrict__ out_index, int32_t* __restrict__ status)
 {
-    typedef TileShape<RT, WN, CHUNKS> S;
+    typedef TileShape<RT, WN, KS, CHUNKS> S;
     constexpr int BN = S::BN, BR = S::BR, XC = S::kRowLoads, CC = S::kCodeLoads;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    char* const code_lds = lds + 2 * S::kRowBytes;
-    char* const scale_lds = code_lds + 2 * S::kCodeBytes;
+    extern __shared__ __attribute__((aligned(16))) char lds_all[];
     report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
     const int n_blocks = (N + BN - 1) / BN;
     TilePlace at;
     if (!find_tile_on_xcd(seg, BR, n_blocks, blockIdx.x, at)) return;
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int lane = lane_id(), wave_all = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int wave = wave_all % WN, share = wave_all / WN;      // of the share
     const int half = lane >> 5, c32 = lane & 31;
     const int nb = at.block * BN;
+    char* const lds = lds_all + share * S::kShareBytes;
+    char* const code_lds = lds + 2 * S::kRowBytes;
+    char* const scale_lds = CHUNKS ? code_lds + 2 * S::kCodeBytes : lds_all + KS * S::kShareBytes;
 
     // Rows in the LDS: 16-byte chunk c of a row's 128 bytes lies at place c ^ (row / 2 % 8).  Codes: chunk c of a row's 64 bytes at
     // place c ^ (bits 2 and 4 of the row).  Reads of 16 rows at a time then touch every bank once.
@@ -170,7 +174,10 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_kernel(const bf16_t* __re
 #pragma unroll
     for (int q = 0; q < 4; ++q) x_off[q] = (c32 * 8 + ((half * 4 + q) ^ ((c32 >> 1) & 7))) * 16;
 
-    const int stages = K / 64;
+    // Stages begin .. end - 1 are this share's: whole pairs, as even as they go.  All shares pass `turns` barriers.
+    const int stages = K / 64, pairs = (stages + 1) / 2;
+    const int begin = 2 * (share * pairs / KS), last_end = 2 * ((share + 1) * pairs / KS);
+    const int end = last_end < stages ? last_end : stages, turns = KS == 1 ? stages : 2 * ((pairs + KS - 1) / KS);
     auto ask_rows = [&](int s, int place) {
 #pragma unroll
         for (int i = 0; i < XC; ++i) {
@@ -199,19 +206,21 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_kernel(const bf16_t* __re
     };
     // ahead of the first stage: scales, codes and rows of stage 0, rows of stage 1, codes of stages 2 and 3
     if constexpr (CHUNKS) {
-        ask_scales(0);
-        if (stages > 8) ask_scales(1);
+        if (begin < end) ask_scales(begin >> 3);
+        if ((begin | 7) + 1 < end) ask_scales((begin >> 3) + 1);
     } else {
         const int there = rows_here * (K / kMxGroup);
-        for (int to = wave * 1024; to < S::scale_bytes(K); to += S::kThreads * 16) {
+        for (int to = wave_all * 1024; to < S::scale_bytes(K); to += KS * S::kThreads * 16) {
             const int mine = to + lane * 16;
             __builtin_amdgcn_global_load_lds(DICEMOE_GLOBAL_PTR(s_base + (mine < there ? mine : 0)), DICEMOE_LDS_PTR(scale_lds + to), 16, 0, 0);
         }
     }
-    ask_codes(0);
-    ask_rows(0, 0);
-    if (stages > 1) ask_rows(1, 1);
-    if (stages > 2) ask_codes(1);
+    if (begin < end) {
+        ask_codes(begin / 2);
+        ask_rows(begin, 0);
+        if (begin + 1 < end) ask_rows(begin + 1, 1);
+        if (begin + 2 < end) ask_codes(begin / 2 + 1);
+    }
     f32x16_v acc[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -230,24 +239,24 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_kernel(const bf16_t* __re
         codes = *reinterpret_cast<const u32x4_t*>(code_lds + ((s >> 1) & 1) * S::kCodeBytes + (c_off ^ (odd * 32)));
         byte = *reinterpret_cast<const uint8_t*>(scale_lds + s_off + (CHUNKS ? ((s >> 3) & 1) * BN * 16 + 2 * (s & 7) : 2 * s));
     };
-    if (stages > 2) wait_vmcnt<XC + CC>();                      // (loads return in order: all but the last ones asked for have landed)
+    if (begin + 2 < end) wait_vmcnt<XC + CC>();                 // (loads return in order: all but the last ones asked for have landed)
     else wait_vmcnt<0>();
     block_barrier();
 
     auto stage = [&](int s, auto odd_tag, auto live_tag) {
         constexpr int ODD = decltype(odd_tag)::value;
         constexpr bool LIVE = decltype(live_tag)::value;
-        const bool more = s + 1 < stages;
+        const bool more = s + 1 < end;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             u32x4_t a;
             if (LIVE) a = u32x4_t{mx4_bf16<0>(codes[q], scale), mx4_bf16<1>(codes[q], scale), mx4_bf16<2>(codes[q], scale), mx4_bf16<3>(codes[q], scale)};
             __builtin_amdgcn_sched_barrier(0);
-            if (q == 3 && more) {
+            if (q == 3 && s + 1 < begin + turns) {
                 wait_lgkmcnt0();                                // this wavefront has read all of stage s, whose place is filled next
                 // The rows of stage s + 1 and all that was asked for before them have landed once only the codes asked for behind them
                 // are under way: behind odd stages codes follow the rows (there are none behind the last rows)
-                if (ODD || s + 2 >= stages) wait_vmcnt<0>();
+                if (ODD || s + 2 >= end) wait_vmcnt<0>();
                 else wait_vmcnt<CC>();
                 block_barrier();
             }
@@ -271,30 +280,51 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_kernel(const bf16_t* __re
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (s + 2 < stages) {
-            if (CHUNKS && ODD && (s & 7) == 7 && s + 9 < stages) ask_scales((s >> 3) + 2);
+        if (s + 2 < end) {
+            if (CHUNKS && ODD && (s & 7) == 7 && s + 9 < end) ask_scales((s >> 3) + 2);
             ask_rows(s + 2, ODD);
-            if (ODD && s + 3 < stages) ask_codes((s + 3) / 2);
+            if (ODD && s + 3 < end) ask_codes((s + 3) / 2);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (LIVE) scale = mx4_scale(byte);
     };
     auto run = [&](auto live_tag) {
         if (decltype(live_tag)::value) {
-            read_weights(0, 0);
+            read_weights(begin, 0);
             read_rows(0, 0, 0);
             scale = mx4_scale(byte);
         }
-        for (int s = 0; s < stages; s += 2) {
+        int s = begin;
+        for (; s < end; s += 2) {
             stage(s, std::integral_constant<int, 0>{}, live_tag);
-            if (s + 1 < stages) stage(s + 1, std::integral_constant<int, 1>{}, live_tag);
+            if (s + 1 < end) stage(s + 1, std::integral_constant<int, 1>{}, live_tag);
         }
+        if (KS > 1)                                             // the barriers of larger shares
+            for (s = end + 1; s < begin + turns; ++s) block_barrier();
     };
-    if (!live) {                                                // columns past N: its loads, waits and barriers only
-        run(std::false_type{});
-        return;
+    if (live && begin < end) run(std::true_type{});
+    else run(std::false_type{});                                // columns past N: its loads, waits and barriers only
+    if constexpr (KS > 1) {                                     // the first share adds the others' sums in order
+        float* const sums = reinterpret_cast<float*>(lds_all);
+        wait_lgkmcnt0();
+        block_barrier();                                        // all stages have been read
+        if (share > 0) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sums[(((share - 1) * RT + r) * 16 + v) * S::kThreads + wave * 64 + lane] = acc[r][v];
+        }
+        wait_lgkmcnt0();
+        block_barrier();
+        if (share > 0) return;
+#pragma unroll
+        for (int o = 0; o < KS - 1; ++o)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[r][v] += sums[((o * RT + r) * 16 + v) * S::kThreads + wave * 64 + lane];
     }
-    run(std::true_type{});
+    if (!live) return;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = at.row0 + r * 32 + c32;
