@@ -103,15 +103,16 @@ __global__ __launch_bounds__(KS * kWave) void mx4_rows_kernel(const T* __restric
 }
 
 // Transposed product of few rows, for the gradient: out[r, k] = sum_n y[r, n] W_e[n, k], times gelu'(u[r, k]) with SLOPE.  A workgroup
-// takes 16 rows and 128 columns k; its four wavefronts share out the reduction in steps of 32 rows of weights.  Lane (g, m) loads, for n =
+// takes 16 rows and 128 columns k; its KS wavefronts share out the reduction in steps of 32 rows of weights.  Lane (g, m) loads, for n =
 // 32 s + 8 g + q (q = 0 .. 7), the dword of codes of columns k = kb + 8 m .. + 7 and their scale; matrix instruction i takes column i
 // of every lane's eight, i.e. its result row 4 g + v stands for column kb + 32 g + 8 v + i.  In bf16 a conversion gives two columns of
 // one n, and pairs along n are put together by byte permutation: one conversion and one permutation per two weights.
-template <typename T, bool SLOPE>
-__global__ __launch_bounds__(256) void mx4_rows_transposed_kernel(const T* __restrict__ y, Segments seg, int N, int K, Mx4 W,
+template <typename T, int KS, bool SLOPE>
+__global__ __launch_bounds__(KS * kWave) void mx4_rows_transposed_kernel(const T* __restrict__ y, Segments seg, int N, int K, Mx4 W,
                                                                   const T* __restrict__ u, T* __restrict__ out, int32_t* __restrict__ status)
 {
-    constexpr int KS = 4, YV = 8 / Store<T>::kVec;
+    constexpr int YV = 8 / Store<T>::kVec;
+    static_assert(KS >= 4, "a thread for every eight results");
     __shared__ f32x4_t red[KS][8][kWave];
     report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
     const int k_blocks = (K + 127) / 128;
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(256) void mx4_rows_transposed_kernel(const T* __res
     // thread (row, column octet): octet 4 g + v of the row's 128 columns
     const int row = threadIdx.x >> 4, octet = threadIdx.x & 15;
     const int ko = kb + octet * 8;
-    if (row0 + row >= row_end || ko >= K) return;
+    if (row0 + row >= row_end || ko >= K || threadIdx.x >= 256) return;
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -275,27 +276,22 @@ int pick_tile(const Segments& seg, int N, int K)
     return best;
 }
 
-// The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns; the LDS does not depend on the reduction).  8192 rows, 4608 -> 1152:
-// 64 x 256 tiles 108 us, 64 x 128 124, 32 x 128 155, 128 x 256 131, 96 x 256 103; 2000 rows 75, 68, 65, 89, 81.
-constexpr int kTilesT = 3, kTileRowsT[kTilesT] = {64, 64, 32}, kTileColumnsT[kTilesT] = {256, 128, 128};
+// The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns of K; its LDS does not depend on the reduction).  4608 -> 1152, 8192
+// rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23.  1152 -> 4608,
+// 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
 template <typename F>
 void with_tile_t(int tile, F&& f)
 {
     if (tile == 0) f(Tile<2, 4, 1>{});
-    else if (tile == 1) f(Tile<2, 2, 1>{});
-    else f(Tile<1, 2, 1>{});
+    else if (tile == 1) f(Tile<1, 2, 2>{});
+    else f(Tile<1, 2, 4>{});
 }
 int pick_tile_t(const Segments& seg, int K)
 {
-    if (seg.max_rows < 16 * seg.n) return -1;
-    constexpr float slow[kTilesT] = {1.0f, 1.25f, 1.6f};
-    int best = 0;
-    float least = 0.f;
-    for (int i = 0; i < kTilesT; ++i) {
-        const float cost = slow[i] * tile_cost(tile_count(seg, kTileRowsT[i], kTileColumnsT[i], K), kTileRowsT[i], kTileColumnsT[i]);
-        if (i == 0 || cost < least) { best = i; least = cost; }
-    }
-    return best;
+    if (seg.max_rows <= 4 * seg.n && tile_bound(seg, 16) * (K / 128) <= 12 * kComputeUnits) return -1;
+    const long long large = tile_count(seg, 64, 256, K), small = tile_count(seg, 32, 128, K);
+    if (tile_cost(large, 64, 256) * (large <= kComputeUnits ? 1.3f : 1.0f) <= 1.6f * tile_cost(small, 32, 128)) return 0;
+    return small <= kComputeUnits ? 2 : 1;
 }
 
 template <typename Shape>
@@ -346,18 +342,25 @@ void transposed_product(const void* y, const Segments& seg, int N, int K, const 
         const int tile = pick_tile_t(seg, K);
         if (tile >= 0) {
             with_tile_t(tile, [&](auto shape) {
-                constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN;
-                typedef TileShapeT<RT, WN> S;
+                constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN, KS = decltype(shape)::KS;
+                typedef TileShapeT<RT, WN, KS> S;
+                static_assert(KS == 4 || S::kLds <= 64 * 1024, "no raised limit");
                 const long long blocks = (tile_bound(seg, S::BR) * ((K + S::BK - 1) / S::BK) + 7) / 8 * 8;
-                hipLaunchKernelGGL((mx4_tile_transposed_kernel<RT, WN, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), S::kLds, stream,
+                hipLaunchKernelGGL((mx4_tile_transposed_kernel<RT, WN, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * S::kThreads), S::kLds, stream,
                                    static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
             });
             return;
         }
     }
-    const long long blocks = tile_bound(seg, 16) * ((K + 127) / 128);
-    hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, static_cast<const T*>(y), seg, N,
-                       K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
+    // Eight shares where each has three steps of 32 at least (float, 1000 rows: 1536 -> 384 33 us against 54 with four; 384 -> 1536 31 against 25)
+    auto go = [&](auto shares) {
+        constexpr int KS = decltype(shares)::value;
+        const long long blocks = tile_bound(seg, 16) * ((K + 127) / 128);
+        hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream,
+                           static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
+    };
+    if (N >= 768) go(std::integral_constant<int, 8>{});
+    else go(std::integral_constant<int, 4>{});
 }
 
 template <typename T>
@@ -389,7 +392,11 @@ hipError_t prepare_expert_ffn_mx4()
     if (err == hipSuccess) err = configure_tile<Tile<2, 4, 1>>();
     if (err == hipSuccess) err = configure_tile<Tile<1, 4, 2>>();
     if (err == hipSuccess) err = configure_tile<Tile<1, 2, 4>>();
-    return err;                                                  // (the transposed tiles need less than the 64 KiB that every kernel has)
+    const auto shares = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<1, 2, 4, false>);
+    const auto shares_slope = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<1, 2, 4, true>);
+    for (const void* kernel : {shares, shares_slope})            // (the other transposed tiles need less than the 64 KiB that every kernel has)
+        if (err == hipSuccess) err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    return err;
 }
 
 hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,

@@ -14,36 +14,38 @@
 
 namespace dicemoe {
 
-template <int RT, int WN> struct TileShapeT {
-    static constexpr int BK = 64 * WN, BR = 32 * RT, kThreads = 64 * WN;
+template <int RT, int WN, int KS> struct TileShapeT {
+    static constexpr int BK = 64 * WN, BR = 32 * RT, kThreads = 64 * WN;            // (of one share)
     static constexpr int kRowBytes = BR * 128, kCodePitch = BK / 2, kCodeBytes = 64 * kCodePitch;
     static constexpr int kScalePitch = 80, kScaleBytes = 2 * WN * kScalePitch * 4;        // (64 floats and 16 more: two groups and two halves on banks of their own)
     static constexpr int kRowLoads = kRowBytes / 16 / kThreads, kCodeLoads = kCodeBytes / 16 / kThreads;
     static_assert(kRowBytes % (16 * kThreads) == 0 && kCodeBytes % (16 * kThreads) == 0, "whole loads");
-    static constexpr int kLds = 2 * (kRowBytes + kCodeBytes + kScaleBytes);
-    static_assert(kLds <= 64 * 1024, "no raised limit");
+    static constexpr int kShareBytes = 2 * (kRowBytes + kCodeBytes + kScaleBytes), kSumBytes = (KS - 1) * 2 * RT * 64 * kThreads;
+    static constexpr int kLds = KS * kShareBytes > kSumBytes ? KS * kShareBytes : kSumBytes;
     // 16-byte chunk c of row n of the codes lies at place c ^ swizzle(n): transposing reads of 16 rows then spread over all banks
     __device__ static constexpr int swizzle(int n) { return WN == 8 ? 2 * (n & 7) : WN == 4 ? (n >> 1) & 7 : (n >> 2) & 3; }
 };
 
-template <int RT, int WN, bool SLOPE>
-__global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const bf16_t* __restrict__ y, Segments seg, int N, int K, Mx4 W,
+template <int RT, int WN, int KS, bool SLOPE>
+__global__ __launch_bounds__(64 * WN * KS, 2) void mx4_tile_transposed_kernel(const bf16_t* __restrict__ y, Segments seg, int N, int K, Mx4 W,
                                                                       const bf16_t* __restrict__ u, bf16_t* __restrict__ out,
                                                                       int32_t* __restrict__ status)
 {
-    typedef TileShapeT<RT, WN> S;
+    typedef TileShapeT<RT, WN, KS> S;
     typedef int i32x2_t __attribute__((ext_vector_type(2)));
     constexpr int BR = S::BR, XC = S::kRowLoads, CC = S::kCodeLoads, PLACES = S::kCodePitch / 16;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    char* const code_lds = lds + 2 * S::kRowBytes;
-    char* const scale_lds = code_lds + 2 * S::kCodeBytes;
+    extern __shared__ __attribute__((aligned(16))) char lds_all[];
     report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
     const int k_blocks = (K + S::BK - 1) / S::BK;
     TilePlace at;
     if (!find_tile_on_xcd(seg, BR, k_blocks, blockIdx.x, at)) return;
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int lane = lane_id(), wave_all = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int wave = wave_all % WN, share = wave_all / WN;      // of the share
     const int half = lane >> 5, c32 = lane & 31;
     const int kb = at.block * S::BK;
+    char* const lds = lds_all + share * S::kShareBytes;
+    char* const code_lds = lds + 2 * S::kRowBytes;
+    char* const scale_lds = code_lds + 2 * S::kCodeBytes;
 
     uint32_t x_from[XC], c_from[CC];
 #pragma unroll
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
     const char* const y_base = reinterpret_cast<const char*>(y);
     const char* const c_base = reinterpret_cast<const char*>(W.codes) + first * (K / 2) + kb / 2;
     // scales: thread (n, pair) stages two groups of row n
-    const int sn = threadIdx.x / WN, spair = threadIdx.x % WN;
+    const int sn = (wave * kWave + lane) / WN, spair = (wave * kWave + lane) % WN;
     const uint8_t* const s_base = W.scales + (first + sn) * (K / kMxGroup) + kb / kMxGroup + (kb + 64 * spair < K ? 2 * spair : 0);
     float* const s_to = reinterpret_cast<float*>(scale_lds) + 2 * spair * S::kScalePitch + sn;
 
@@ -72,7 +74,10 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
 #pragma unroll
     for (int q = 0; q < 4; ++q) x_off[q] = (c32 * 8 + ((q * 2 + half) ^ ((c32 >> 1) & 7))) * 16;
 
-    const int stages = N / 64;
+    // Stages begin .. end - 1 are this share's: whole pairs, as even as they go.  All shares pass `turns` barriers.
+    const int stages = N / 64, pairs = (stages + 1) / 2;
+    const int begin = 2 * (share * pairs / KS), last_end = 2 * ((share + 1) * pairs / KS);
+    const int end = last_end < stages ? last_end : stages, turns = KS == 1 ? stages : 2 * ((pairs + KS - 1) / KS);
     auto ask = [&](int s, int place) {
 #pragma unroll
         for (int i = 0; i < XC; ++i) {
@@ -95,12 +100,16 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
         s_to[place * (S::kScaleBytes / 4) + S::kScalePitch] = mx4_scale(two >> 8);
     };
     uint32_t two[2];                                            // scales on their way, by the parity of their stage
-    const uint32_t two0 = ask_scales(0);
-    two[1] = stages > 1 ? ask_scales(1) : 0u;
-    two[0] = stages > 2 ? ask_scales(2) : 0u;
-    ask(0, 0);
-    if (stages > 1) ask(1, 1);
-    keep_scales(two0, 0);
+    uint32_t two0 = 0u;
+    two[0] = two[1] = 0u;
+    if (begin < end) {
+        two0 = ask_scales(begin);
+        if (begin + 1 < end) two[1] = ask_scales(begin + 1);
+        if (begin + 2 < end) two[0] = ask_scales(begin + 2);
+        ask(begin, 0);
+        if (begin + 1 < end) ask(begin + 1, 1);
+        keep_scales(two0, 0);
+    }
     f32x16_v acc[2][RT];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -129,7 +138,7 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
         scale[0] = from[0];
         scale[1] = from[1];
     };
-    if (stages > 1) wait_vmcnt<XC + CC>();                      // (loads return in order: all but stage 1's have landed)
+    if (begin + 1 < end) wait_vmcnt<XC + CC>();                 // (loads return in order: all but stage 1's have landed)
     else wait_vmcnt<0>();
     wait_lgkmcnt0();
     block_barrier();
@@ -137,7 +146,7 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
     auto stage = [&](int s, auto odd_tag, auto live_tag) {
         constexpr int ODD = decltype(odd_tag)::value;
         constexpr bool LIVE = decltype(live_tag)::value;
-        const bool more = s + 1 < stages;
+        const bool more = s + 1 < end;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             u32x4_t a[2];
@@ -153,7 +162,7 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
             }
             __builtin_amdgcn_sched_barrier(0);
             if (q == 2 && more) keep_scales(two[1 - ODD], 1 - ODD);      // of stage s + 1, asked for two stages ago
-            if (q == 3 && more) {
+            if (q == 3 && s + 1 < begin + turns) {
                 wait_lgkmcnt0();                                // this wavefront has read all of stage s, whose place is filled next
                 wait_vmcnt<0>();                                // its loads of stage s + 1, asked for a stage ago, have landed
                 block_barrier();
@@ -181,8 +190,8 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (s + 3 < stages) two[1 - ODD] = ask_scales(s + 3);
-        if (s + 2 < stages) ask(s + 2, ODD);
+        if (s + 3 < end) two[1 - ODD] = ask_scales(s + 3);
+        if (s + 2 < end) ask(s + 2, ODD);
         __builtin_amdgcn_sched_barrier(0);
     };
     auto run = [&](auto live_tag) {
@@ -191,16 +200,37 @@ __global__ __launch_bounds__(64 * WN, 2) void mx4_tile_transposed_kernel(const b
             read_scales(0, 0);
             read_rows(0, 0, 0);
         }
-        for (int s = 0; s < stages; s += 2) {
+        int s = begin;
+        for (; s < end; s += 2) {
             stage(s, std::integral_constant<int, 0>{}, live_tag);
-            if (s + 1 < stages) stage(s + 1, std::integral_constant<int, 1>{}, live_tag);
+            if (s + 1 < end) stage(s + 1, std::integral_constant<int, 1>{}, live_tag);
         }
+        if (KS > 1)                                             // the barriers of larger shares
+            for (s = end + 1; s < begin + turns; ++s) block_barrier();
     };
-    if (!live) {                                                // columns past K: its loads, waits and barriers only
-        run(std::false_type{});
-        return;
+    if (live && begin < end) run(std::true_type{});
+    else run(std::false_type{});                                // columns past K: its loads, waits and barriers only
+    if constexpr (KS > 1) {                                     // the first share adds the others' sums in order
+        float* const sums = reinterpret_cast<float*>(lds_all);
+        wait_lgkmcnt0();
+        block_barrier();                                        // all stages have been read
+        if (share > 0) {
+#pragma unroll
+            for (int i = 0; i < 2 * RT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sums[(((share - 1) * 2 * RT + i) * 16 + v) * S::kThreads + wave * kWave + lane] = acc[i / RT][i % RT][v];
+        }
+        wait_lgkmcnt0();
+        block_barrier();
+        if (share > 0) return;
+#pragma unroll
+        for (int o = 0; o < KS - 1; ++o)
+#pragma unroll
+            for (int i = 0; i < 2 * RT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i / RT][i % RT][v] += sums[((o * 2 * RT + i) * 16 + v) * S::kThreads + wave * kWave + lane];
     }
-    run(std::true_type{});
+    if (!live) return;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = at.row0 + r * 32 + c32;
