@@ -8,7 +8,6 @@ library is missing the import of this module's functions fails loudly.
 from __future__ import annotations
 
 import ctypes
-import math
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -268,13 +267,15 @@ class Context:
                                       _ptr(H_cache, self.torch_dtype), _ptr(S_cache, torch.float32),
                                       int(bool(use_fresh_scores)), _ptr(y, self.torch_dtype), _stream()))
 
-    def _sized(self, name, t, dtype, *shape):
-        """The address of a contiguous tensor of exactly this many elements (None stays None)."""
-        if t is not None and t.numel() != math.prod(shape):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    @staticmethod
+    def _sized(name, t, dtype, n):
+        """The address of a contiguous tensor of exactly n elements (None stays None)."""
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {n} elements")
         return _ptr(t, dtype)
 
-    def _rows(self, name, t, dtype, rows, cols):
+    @staticmethod
+    def _rows(name, t, dtype, rows, cols):
         """The address of a contiguous tensor of at least ``rows`` rows of ``cols`` columns."""
         if t is not None and (t.shape[-1] != cols or t.numel() < rows * cols):
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected at least {rows} rows of {cols}")
@@ -282,17 +283,23 @@ class Context:
 
     def _mx4(self, name, weights, rows, cols):
         codes, scales = weights
-        return (self._sized(f"{name} codes", codes, torch.uint8, self.experts, rows, cols // 2),
-                self._sized(f"{name} scales", scales, torch.uint8, self.experts, rows, cols // 32))
+        n = self.experts * rows * cols
+        return self._sized(name, codes, torch.uint8, n // 2), self._sized(name, scales, torch.uint8, n // 32)
+
+    @staticmethod
+    def _pairs(name, t, n):
+        if t is not None and t.numel() < n:
+            raise ValueError(f"{name} has {t.numel()} entries, expected at least {n}")
+        return _ptr(t, torch.int32)
 
     def moe_quantize_mx4(self, W, codes, scales, values=None):
         """W [..., cols] to MXFP4 codes [..., cols / 2] and scale bytes [..., cols / 32]; ``values``: what they stand for."""
         cols = W.shape[-1]
         rows = W.numel() // cols if cols else 0
         self._check(lib().moe_quantize_mx4(self._h, _ptr(W, self.torch_dtype), rows, cols,
-                                           self._sized("codes", codes, torch.uint8, rows, cols // 2),
-                                           self._sized("scales", scales, torch.uint8, rows, cols // 32),
-                                           self._sized("values", values, self.torch_dtype, rows, cols), _stream()))
+                                           self._sized("codes", codes, torch.uint8, rows * (cols // 2)),
+                                           self._sized("scales", scales, torch.uint8, rows * (cols // 32)),
+                                           self._sized("values", values, self.torch_dtype, rows * cols), _stream()))
 
     def moe_expert_ffn_mx4(self, x_rows, row_pairs, out_pairs, seg_offsets, seg_expert, max_rows, W1, b1, W2, b2, u_packed, h_rows,
                            workspace):
@@ -300,11 +307,11 @@ class Context:
         ``row_pairs``, ``out_pairs`` and ``u_packed`` may be None."""
         st, d, F, n_seg = self.torch_dtype, self.d, self.F, seg_expert.shape[0]
         self._check(lib().moe_expert_ffn_mx4(
-            self._h, self._rows("x_rows", x_rows, st, max_rows if row_pairs is None else 0, d), _ptr(row_pairs, torch.int32),
-            _ptr(out_pairs, torch.int32),
-            self._sized("seg_offsets", seg_offsets, torch.int32, n_seg + 1), _ptr(seg_expert, torch.int32), n_seg, max_rows,
-            *self._mx4("W1", W1, F, d), self._sized("b1", b1, torch.float32, self.experts, F),
-            *self._mx4("W2", W2, d, F), self._sized("b2", b2, torch.float32, self.experts, d),
+            self._h, self._rows("x_rows", x_rows, st, max_rows if row_pairs is None else 0, d), self._pairs("row_pairs", row_pairs, max_rows),
+            self._pairs("out_pairs", out_pairs, max_rows),
+            self._pairs("seg_offsets", seg_offsets, n_seg + 1), _ptr(seg_expert, torch.int32), n_seg, max_rows,
+            *self._mx4("W1", W1, F, d), self._sized("b1", b1, torch.float32, self.experts * F),
+            *self._mx4("W2", W2, d, F), self._sized("b2", b2, torch.float32, self.experts * d),
             self._rows("u_packed", u_packed, st, max_rows, F), self._rows("h_rows", h_rows, st, 0 if out_pairs is not None else max_rows, d),
             _ptr(workspace), _stream()))
 
@@ -314,29 +321,30 @@ class Context:
         st, d, F, n_seg = self.torch_dtype, self.d, self.F, seg_expert.shape[0]
         self._check(lib().moe_expert_ffn_mx4_backward(
             self._h, self._rows("dh_packed", dh_packed, st, max_rows, d), self._rows("u_packed", u_packed, st, max_rows, F),
-            self._sized("seg_offsets", seg_offsets, torch.int32, n_seg + 1), _ptr(seg_expert, torch.int32), n_seg, max_rows,
+            self._pairs("seg_offsets", seg_offsets, n_seg + 1), _ptr(seg_expert, torch.int32), n_seg, max_rows,
             *self._mx4("W1", W1, F, d), *self._mx4("W2", W2, d, F), self._rows("du_packed", du_packed, st, max_rows, F),
             self._rows("dx_packed", dx_packed, st, max_rows, d), _ptr(workspace), _stream()))
 
     def moe_combine_backward(self, dy, h_packed, inv, scores, dh_packed, dscores):
         """Gradient of moe_combine without caches: rows ``dh_packed`` and float ``dscores``."""
-        st, T, d, k = self.torch_dtype, dy.shape[0], self.d, self.slots
+        st, f32, T, d = self.torch_dtype, torch.float32, dy.shape[0], self.d
+        N = T * self.slots
         self._check(lib().moe_combine_backward(
-            self._h, self._sized("dy", dy, st, T, d), self._rows("h_packed", h_packed, st, 0, d),
-            self._rows("inv", inv.view(-1, 1), torch.int32, T * k, 1), self._sized("scores", scores, torch.float32, T, k), T,
-            self._rows("dh_packed", dh_packed, st, h_packed.shape[0], d), self._sized("dscores", dscores, torch.float32, T, k), _stream()))
+            self._h, self._sized("dy", dy, st, T * d), self._rows("h_packed", h_packed, st, 0, d), self._pairs("inv", inv, N),
+            self._sized("scores", scores, f32, N), T, self._rows("dh_packed", dh_packed, st, h_packed.numel() // d, d),
+            self._sized("dscores", dscores, f32, N), _stream()))
 
     def moe_route_backward(self, x, Wg, expert_idx, probs_all, dscores, dprobs, dlogits, dx_packed, inv, dx, dz, dWg, dbg, workspace):
         """Gradient of moe_gate and moe_dispatch.  ``dprobs``, ``dlogits``, ``dz``, ``dWg``, ``dbg`` may be None, ``dx_packed``
         and ``inv`` together (the router alone); with ``Wg`` None it is the gradient of the dispatch alone."""
-        st, f32, i32, T, d, E, k = self.torch_dtype, torch.float32, torch.int32, dx.shape[0], self.d, self.E, self.slots
+        st, f32, T, d, E, sized = self.torch_dtype, torch.float32, dx.shape[0], self.d, self.E, self._sized
+        N = T * self.slots
         self._check(lib().moe_route_backward(
-            self._h, self._sized("x", x, st, T, d), self._sized("Wg", Wg, st, E, d), self._sized("expert_idx", expert_idx, i32, T, k),
-            self._sized("probs_all", probs_all, f32, T, E), self._sized("dscores", dscores, f32, T, k),
-            self._sized("dprobs", dprobs, f32, T, E), self._sized("dlogits", dlogits, f32, T, E),
-            self._rows("dx_packed", dx_packed, st, 0, d), None if inv is None else self._rows("inv", inv.view(-1, 1), i32, T * k, 1), T,
-            self._sized("dx", dx, st, T, d), self._sized("dz", dz, f32, T, E), self._sized("dWg", dWg, f32, E, d),
-            self._sized("dbg", dbg, f32, E), _ptr(workspace), _stream()))
+            self._h, sized("x", x, st, T * d), sized("Wg", Wg, st, E * d), sized("expert_idx", expert_idx, torch.int32, N),
+            sized("probs_all", probs_all, f32, T * E), sized("dscores", dscores, f32, N), sized("dprobs", dprobs, f32, T * E),
+            sized("dlogits", dlogits, f32, T * E), self._rows("dx_packed", dx_packed, st, 0, d), self._pairs("inv", inv, N), T,
+            sized("dx", dx, st, T * d), sized("dz", dz, f32, T * E), sized("dWg", dWg, f32, E * d), sized("dbg", dbg, f32, E),
+            _ptr(workspace), _stream()))
 
     def moe_ep_segments(self, recv_counts, seg_offsets, seg_expert):
         W, E_loc = recv_counts.shape

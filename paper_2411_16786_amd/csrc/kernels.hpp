@@ -115,7 +115,7 @@ hipError_t launch_combine_backward(bool bf16, const void* dy, const void* h_pack
                                    int d, int k, void* dh_packed, float* dscores, hipStream_t stream);
 
 // Gradient of router and dispatch (Wg null: of the dispatch alone).  slots: columns of idx, dscores and inv, the first k of them routed.
-// partial, partial_dbg: set by the launcher, in a workspace of route_backward_bytes(T, E, d) bytes.
+// partial, partial_dbg (and dz, where it is null): set by the launcher, in a workspace of route_backward_bytes(T, E, d) bytes.
 struct RouteBackward {
     const void *x, *Wg;
     const int32_t* idx;

@@ -4,6 +4,7 @@
 //   dz   = P (g - <P, g>) + the logits' own gradient
 //   dx_i = sum_j dx_packed[inv_ij]  +  sum_e dz_ie Wg_e          (float, slots in order, rounded once)
 //   dWg  = dz^T x,   dbg = sum_i dz_i                            (float)
+#include <type_traits>
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -48,103 +49,160 @@ __global__ __launch_bounds__(256) void dispatch_backward_kernel(const T* __restr
     }
 }
 
-// A workgroup takes `chunk` tokens (a multiple of 16) and 16 x kVec columns.  It first forms dz of its tokens in LDS (16 lanes per
-// token, one expert each and 16 apart), then its four wavefronts take tiles of 16 tokens.  Both products run on float matrix
-// instructions (16x16x4: exact products, float sums), chosen so that one 16-byte load per lane feeds them in place: lane (g, m) =
-// (l / 16, l % 16) loads columns c0 + m V .. of token 4g + v (row g of step v for dz^T x) or of expert 4s + g (step s of dz Wg),
-// and component j of the 16 bytes is the operand of instruction j.  The result of dz Wg then has V consecutive columns of
-// tokens 4g .. 4g + 3 in the lane that also gathers the dispatch's rows for them and stores 16 bytes.
-// dz^T x stays in registers over a wavefront's tiles; the four meet in LDS in wavefront order, and workgroups write partial sums
-// [token chunk][E][d] that route_backward_sum_kernel adds in chunk order (one chunk: straight to the result).
-template <typename T, int NB>
-__global__ __launch_bounds__(256) void route_backward_kernel(RouteBackward a, int chunk, int columns, int chunks)
+// dz: 16 lanes per token, lane m with the experts m, m + 16, ..
+template <int NB>
+__global__ __launch_bounds__(256) void route_logits_kernel(RouteBackward a)
 {
-    constexpr int V = Store<T>::kVec, EP = 16 * NB;
-    extern __shared__ float lds[];                   // dz[chunk][EP], later the four wavefronts' sums of one block of experts
+    const int lane = lane_id(), m = lane & 15;
+    const int at = blockIdx.x * 16 + threadIdx.x / 16, tok = at < a.T ? at : a.T - 1;
+    const size_t te = static_cast<size_t>(tok) * a.E, tk = static_cast<size_t>(tok) * a.slots;
+    float P[NB], ge[NB], dl[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int e = m + 16 * b;
+        const bool on = e < a.E;
+        P[b] = on ? a.probs[te + e] : 0.f;
+        ge[b] = on && a.dprobs != nullptr ? a.dprobs[te + e] : 0.f;
+        dl[b] = on && a.dlogits != nullptr ? a.dlogits[te + e] : 0.f;
+    }
+    float total = 1.f, mean = 0.f;
+    if (a.renorm) {
+        total = 0.f;
+        for (int j = 0; j < a.k; ++j) {
+            const float p = a.probs[te + a.idx[tk + j]];
+            total += p;
+            mean = fmaf(a.dscores[tk + j], p, mean);
+        }
+        mean /= total;
+    }
+    for (int j = 0; j < a.k; ++j) {
+        const int e = a.idx[tk + j];
+        const float add = (a.dscores[tk + j] - mean) / total;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            if (e == m + 16 * b) ge[b] += add;
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) dot = fmaf(P[b], ge[b], dot);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) dot += __shfl_xor(dot, o, kWave);
+    if (at >= a.T) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+        if (m + 16 * b < a.E) a.dz[te + m + 16 * b] = P[b] * (ge[b] - dot) + dl[b];
+}
+
+// A workgroup takes `chunk` tokens (a multiple of 64), whose dz it keeps in LDS, and 16 x kVec columns; its four wavefronts take tiles
+// of 16 tokens.  Both products run on float matrix instructions (16x16x4: exact products, float sums), chosen so that one 16-byte load
+// per lane feeds them in place: lane (g, m) = (l / 16, l % 16) loads columns c0 + m V .. of token 4g + v (row g of step v for dz^T x)
+// or of expert 4s + g (step s of dz Wg), and component j of the 16 bytes is the operand of instruction j.  The result of dz Wg then has V
+// consecutive columns of tokens 4g .. 4g + 3 in the lane that also gathers the dispatch's rows for them and stores 16 bytes.  dz^T x stays in registers
+// over a wavefront's tiles; the four meet in LDS in wavefront order, and workgroups write partial sums [token chunk][E][d] that
+// route_backward_sum_kernel adds in chunk order (one chunk: straight to the result).
+// Bound by memory (k + 2 rows per token); what costs is latency, so a tile asks for all of its rows before its first product, and
+// the first one's are under way while dz comes.  Forming dz here, once per column block, took 10 us more (8192 tokens of 2048 columns, 16
+// experts) than the launch of its own.
+// KK > 0: KK slots per token, their rows of a tile in flight together; KK == 0: any number, row by row.
+template <typename T, int NB, int KK>
+__global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(RouteBackward a, int chunk, int columns, int chunks)
+{
+    constexpr int V = Store<T>::kVec, EP = 16 * NB, KN = KK > 0 ? KK : 1;
+    extern __shared__ float lds[];                   // dz[chunk][EP] and 256 more, later the four wavefronts' sums of one block of experts
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     const int m = lane & 15, g = lane >> 4;
     const int part = blockIdx.x / columns, column = blockIdx.x - part * columns;
     const int tok0 = part * chunk, d = a.d, E = a.E;
     const bool first = column == 0;
+    const int c = column * 16 * V + m * V;           // the lane's first column
+    const bool col_on = c < d;
+    const u32x4_t none = {0u, 0u, 0u, 0u};
+    const T* const Wg = static_cast<const T*>(a.Wg);
+    const T* const x = static_cast<const T*>(a.x);
+    const T* const dxp = static_cast<const T*>(a.dx_packed);
+    T* const dx = static_cast<T*>(a.dx);
+    auto router_row = [&](int e) { return col_on && e < E ? *reinterpret_cast<const u32x4_t*>(Wg + static_cast<size_t>(e) * d + c) : none; };
 
-    for (int i = threadIdx.x / 16; i < chunk; i += 16) {
-        const int tok = tok0 + i;
-        const bool on = tok < a.T;
-        const size_t te = static_cast<size_t>(on ? tok : 0) * E, tk = static_cast<size_t>(on ? tok : 0) * a.slots;
-        float P[NB], ge[NB];
+    // what tile t0 reads: packed rows of its tokens first, then the rows themselves and x
+    u32x4_t xv[4], rv[4][KN];
+    int row[4][KN];
+    auto ask_places = [&](int t0) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int e = m + 16 * b;
-            P[b] = e < E ? a.probs[te + e] : 0.f;
-            ge[b] = a.dprobs != nullptr && e < E ? a.dprobs[te + e] : 0.f;
+        for (int v = 0; v < 4; ++v) {
+            const int tok = tok0 + t0 + 4 * g + v;
+#pragma unroll
+            for (int j = 0; j < KN; ++j)
+                row[v][j] = KK > 0 && col_on && tok < a.T && dxp != nullptr ? a.inv[static_cast<size_t>(tok) * KN + j] : -1;
         }
-        float total = 1.f, mean = 0.f;
-        if (a.renorm) {
-            total = 0.f;
-            for (int j = 0; j < a.k; ++j) {
-                const float p = a.probs[te + a.idx[tk + j]];
-                total += p;
-                mean = fmaf(a.dscores[tk + j], p, mean);
+    };
+    auto ask_rows = [&](int t0) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int tok = tok0 + t0 + 4 * g + v;
+#pragma unroll
+            for (int j = 0; j < KN; ++j) rv[v][j] = row[v][j] >= 0 ? *reinterpret_cast<const u32x4_t*>(dxp + static_cast<size_t>(row[v][j]) * d + c) : none;
+            xv[v] = col_on && tok < a.T && a.dWg != nullptr ? *reinterpret_cast<const u32x4_t*>(x + static_cast<size_t>(tok) * d + c) : none;
+        }
+    };
+    ask_places(wave * 16);
+    {
+        float dz[4];
+        int i0 = threadIdx.x;
+        auto ask_dz = [&]() {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + 256 * u, tok = tok0 + i / EP, e = i % EP;
+                dz[u] = tok < a.T && e < E ? a.dz[static_cast<size_t>(tok) * E + e] : 0.f;      // what only fills up a tile adds nothing
             }
-            mean /= total;
-        }
-        for (int j = 0; j < a.k; ++j) {
-            const int e = a.idx[tk + j];
-            const float ds = (a.dscores[tk + j] - mean) / total;
+        };
+        auto keep_dz = [&]() {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-                if (e == m + 16 * b) ge[b] += ds;
-        }
-        float dot = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) dot = fmaf(P[b], ge[b], dot);
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) dot += __shfl_xor(dot, x, kWave);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int e = m + 16 * b;
-            float dz = P[b] * (ge[b] - dot);
-            if (a.dlogits != nullptr && e < E) dz += a.dlogits[te + e];
-            if (!on || e >= E) dz = 0.f;             // tokens and experts that only fill up a tile add nothing
-            lds[i * EP + e] = dz;
-            if (first && a.dz != nullptr && on && e < E) a.dz[te + e] = dz;
+            for (int u = 0; u < 4; ++u) lds[i0 + 256 * u] = dz[u];
+        };
+        ask_dz();
+        ask_rows(wave * 16);                         // (loads return in order: behind the first that LDS waits for)
+        keep_dz();
+        for (i0 += 1024; i0 < chunk * EP; i0 += 1024) {
+            ask_dz();
+            keep_dz();
         }
     }
     __syncthreads();
-    if (first && a.dbg != nullptr && threadIdx.x < E) {
-        float sum = 0.f;
-        for (int i = 0; i < chunk; ++i) sum += lds[i * EP + threadIdx.x];
-        (chunks == 1 ? a.dbg : a.partial_dbg + static_cast<size_t>(part) * E)[threadIdx.x] = sum;
+    if (first && a.dbg != nullptr) {                 // (thread: expert t % EP, every 256 / EP-th token from t / EP on)
+        float* const sums = lds + chunk * EP;
+        const int e = static_cast<int>(threadIdx.x) % EP, from = static_cast<int>(threadIdx.x) / EP;
+        constexpr int STEP = 256 / EP;
+        if (from < STEP) {
+            float sum = 0.f;
+#pragma unroll 4
+            for (int i = from; i < chunk; i += STEP) sum += lds[i * EP + e];
+            sums[from * EP + e] = sum;
+        }
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < E) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) sum += sums[i * EP + threadIdx.x];
+            (chunks == 1 ? a.dbg : a.partial_dbg + static_cast<size_t>(part) * E)[threadIdx.x] = sum;
+        }
     }
 
-    const int c = column * 16 * V + m * V;       // the lane's first column
-    const bool col_on = c < d;
-    const u32x4_t none = {0u, 0u, 0u, 0u};
     f32x4_t accW[NB][V];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < V; ++j) accW[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const T* const Wg = static_cast<const T*>(a.Wg);
-    const T* const x = static_cast<const T*>(a.x);
-    const T* const dxp = static_cast<const T*>(a.dx_packed);
-    T* const dx = static_cast<T*>(a.dx);
     for (int t0 = wave * 16; t0 < chunk && tok0 + t0 < a.T; t0 += 64) {
-        u32x4_t xv[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int tok = tok0 + t0 + 4 * g + v;
-            xv[v] = a.dWg != nullptr && col_on && tok < a.T ? *reinterpret_cast<const u32x4_t*>(x + static_cast<size_t>(tok) * d + c) : none;
-        }
+        const int tok = tok0 + t0 + 4 * g;           // the lane's first token
         f32x4_t accX[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) accX[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int e0 = 0; e0 < E; e0 += 4) {
-            const int e = e0 + g;
-            const u32x4_t wv = col_on && e < E ? *reinterpret_cast<const u32x4_t*>(Wg + static_cast<size_t>(e) * d + c) : none;
-            const float dz = lds[(t0 + m) * EP + e];
+#pragma unroll
+        for (int s = 0; s < 4 * NB; ++s) {           // (experts past E: dz and the router's row are zero)
+            const u32x4_t row = router_row(4 * s + g);
+            const float dz = lds[(t0 + m) * EP + 4 * s + g];
             float w[V];
-            Store<T>::unpack(wv, w);
+            Store<T>::unpack(row, w);
 #pragma unroll
             for (int j = 0; j < V; ++j) accX[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(dz, w[j], accX[j], 0, 0, 0);
         }
@@ -163,24 +221,33 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackward a, in
         }
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int tok = tok0 + t0 + 4 * g + v;
-            if (tok >= a.T || !col_on) continue;
+            if (tok + v >= a.T || !col_on) continue;
             float sum[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) sum[j] = 0.f;
-            if (dxp != nullptr)
-                for (int j = 0; j < a.slots; ++j) {
-                    const int row = a.inv[static_cast<size_t>(tok) * a.slots + j];
-                    if (row < 0) continue;
-                    float f[V];
-                    Store<T>::unpack(*reinterpret_cast<const u32x4_t*>(dxp + static_cast<size_t>(row) * d + c), f);
+            auto add = [&](const u32x4_t& row) {
+                float f[V];
+                Store<T>::unpack(row, f);
 #pragma unroll
-                    for (int t = 0; t < V; ++t) sum[t] += f[t];
+                for (int t = 0; t < V; ++t) sum[t] += f[t];
+            };
+            if (KK > 0) {
+#pragma unroll
+                for (int j = 0; j < KN; ++j) add(rv[v][j]);
+            } else if (dxp != nullptr) {
+                for (int j = 0; j < a.slots; ++j) {
+                    const int row = a.inv[static_cast<size_t>(tok + v) * a.slots + j];
+                    if (row >= 0) add(*reinterpret_cast<const u32x4_t*>(dxp + static_cast<size_t>(row) * d + c));
                 }
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) sum[j] += accX[j][v];
             const uint4 packed = Store<T>::pack(sum);
-            *reinterpret_cast<u32x4_t*>(dx + static_cast<size_t>(tok) * d + c) = u32x4_t{packed.x, packed.y, packed.z, packed.w};
+            *reinterpret_cast<u32x4_t*>(dx + static_cast<size_t>(tok + v) * d + c) = u32x4_t{packed.x, packed.y, packed.z, packed.w};
+        }
+        if (t0 + 64 < chunk) {
+            ask_places(t0 + 64);
+            ask_rows(t0 + 64);
         }
     }
     if (a.dWg == nullptr) return;
@@ -210,26 +277,39 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackward a, in
     }
 }
 
-// out[i] = sum over the token chunks of partial[chunk][i], in chunk order, for the n = E d values of dWg and then the E of dbg
+// dWg[i] = sum over the token chunks of partial[chunk][i] for its n = E d values, four at a time, and the E values of dbg (by the last
+// workgroup).  Eight threads share out the chunks of a place, so that their loads do not wait for one another, and add up in LDS; the
+// order is fixed.
 __global__ __launch_bounds__(256) void route_backward_sum_kernel(const float* __restrict__ partial, const float* __restrict__ partial_dbg,
                                                                  int chunks, int n, int E, float* __restrict__ dWg, float* __restrict__ dbg)
 {
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < n && dWg != nullptr) {
-        float sum = 0.f;
-        for (int c = 0; c < chunks; ++c) sum += partial[static_cast<size_t>(c) * n + i];
-        dWg[i] = sum;
+    __shared__ f32x4_t sums[8][32];
+    const int place = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const int i = (blockIdx.x * 32 + place) * 4;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    if (dWg != nullptr && i < n)
+        for (int c = share; c < chunks; c += 8) sum += *reinterpret_cast<const f32x4_t*>(partial + static_cast<size_t>(c) * n + i);
+    sums[share][place] = sum;
+    __syncthreads();
+    if (share == 0 && dWg != nullptr && i < n) {
+#pragma unroll
+        for (int q = 1; q < 8; ++q) sum += sums[q][place];
+        *reinterpret_cast<f32x4_t*>(dWg + i) = sum;
     }
-    if (i < E && dbg != nullptr) {
-        float sum = 0.f;
-        for (int c = 0; c < chunks; ++c) sum += partial_dbg[static_cast<size_t>(c) * E + i];
-        dbg[i] = sum;
-    }
+    if (dbg == nullptr || blockIdx.x != gridDim.x - 1) return;
+    float total = 0.f;                               // thread (share t / 64, expert t % 64)
+    __shared__ float totals[4][64];
+    const int e = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+    if (e < E)
+        for (int c = quarter; c < chunks; c += 4) total += partial_dbg[static_cast<size_t>(c) * E + e];
+    totals[quarter][e] = total;
+    __syncthreads();
+    if (quarter == 0 && e < E) dbg[e] = (total + totals[1][e]) + (totals[2][e] + totals[3][e]);
 }
 
 namespace {
 
-// Tokens per workgroup: 64, one tile per wavefront, while that leaves a workgroup or less per compute unit; then up to 256 (128 with more
+// Tokens per workgroup: 64, one tile per wavefront, while that leaves two workgroups or less per compute unit; then up to 256 (128 with more
 // than 32 experts, whose dz has to fit the LDS), which keeps the partial sums a small part of what is read.
 int route_chunk(int T_tok, int E, int columns)
 {
@@ -241,9 +321,16 @@ int route_chunk(int T_tok, int E, int columns)
 template <typename T, int NB>
 void launch_route_backward_t(const RouteBackward& a, int columns, int chunk, int chunks, hipStream_t stream)
 {
-    const int dz = chunk * 16 * NB, sums = 4 * 4 * Store<T>::kVec * kWave;
-    hipLaunchKernelGGL((route_backward_kernel<T, NB>), dim3(columns * chunks), dim3(256), (dz > sums ? dz : sums) * sizeof(float),
-                       stream, a, chunk, columns, chunks);
+    const int dz = chunk * 16 * NB + 256, sums = 4 * 4 * Store<T>::kVec * kWave;
+    const size_t lds = (dz > sums ? dz : sums) * sizeof(float);
+#define DICEMOE_ROUTE_BWD_K(KK_) \
+    hipLaunchKernelGGL((route_backward_kernel<T, NB, KK_>), dim3(columns * chunks), dim3(256), lds, stream, a, chunk, columns, chunks)
+    if (a.slots == 1) DICEMOE_ROUTE_BWD_K(1);
+    else if (a.slots == 2) DICEMOE_ROUTE_BWD_K(2);
+    else if (a.slots == 3) DICEMOE_ROUTE_BWD_K(3);
+    else if (a.slots == 4) DICEMOE_ROUTE_BWD_K(4);
+    else DICEMOE_ROUTE_BWD_K(0);
+#undef DICEMOE_ROUTE_BWD_K
 }
 
 template <typename T>
@@ -263,9 +350,10 @@ void launch_dispatch_backward_t(const RouteBackward& a, hipStream_t stream)
 
 }  // namespace
 
+// partial sums by chunks of 64 tokens or more, and dz if the caller does not want it
 size_t route_backward_bytes(long long T_max, int E, int d)
 {
-    return static_cast<size_t>((T_max + 63) / 64) * E * (static_cast<size_t>(d) + 1) * sizeof(float);
+    return (static_cast<size_t>((T_max + 63) / 64) * E * (static_cast<size_t>(d) + 1) + static_cast<size_t>(T_max) * E) * sizeof(float);
 }
 
 hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hipStream_t stream)
@@ -280,8 +368,15 @@ hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hi
     const int chunk = route_chunk(a.T, a.E, columns), chunks = (a.T + chunk - 1) / chunk;
     a.partial = static_cast<float*>(workspace);
     a.partial_dbg = a.partial + static_cast<size_t>(chunks) * a.E * a.d;
+    if (a.dz == nullptr) a.dz = a.partial_dbg + static_cast<size_t>(chunks) * a.E;
     if (chunks > 0) {
         const int blocks = (a.E + 15) / 16;
+        auto logits = [&](auto nb) { hipLaunchKernelGGL(route_logits_kernel<decltype(nb)::value>, dim3((a.T + 15) / 16), dim3(256), 0, stream, a); };
+        if (blocks == 1) logits(std::integral_constant<int, 1>{});
+        else if (blocks == 2) logits(std::integral_constant<int, 2>{});
+        else if (blocks == 3) logits(std::integral_constant<int, 3>{});
+        else logits(std::integral_constant<int, 4>{});
+        if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
 #define DICEMOE_ROUTE_BWD(T_)                                                             \
     do {                                                                                  \
         if (blocks == 1) launch_route_backward_t<T_, 1>(a, columns, chunk, chunks, stream);      \
@@ -296,7 +391,7 @@ hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hi
     }
     if (chunks == 1 || (a.dWg == nullptr && a.dbg == nullptr)) return hipSuccess;
     const int n = a.E * a.d;                         // (no token: the sums are zeros)
-    hipLaunchKernelGGL(route_backward_sum_kernel, dim3((n + 255) / 256), dim3(256), 0, stream, a.partial, a.partial_dbg, chunks, n, a.E, a.dWg, a.dbg);
+    hipLaunchKernelGGL(route_backward_sum_kernel, dim3((n + 127) / 128), dim3(256), 0, stream, a.partial, a.partial_dbg, chunks, n, a.E, a.dWg, a.dbg);
     return hipGetLastError();
 }
 
