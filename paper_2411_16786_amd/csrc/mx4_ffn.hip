@@ -103,41 +103,42 @@ __global__ __launch_bounds__(KS * kWave) void mx4_rows_kernel(const T* __restric
 }
 
 // Transposed product of few rows, for the gradient: out[r, k] = sum_n y[r, n] W_e[n, k], times gelu'(u[r, k]) with SLOPE.  A workgroup
-// takes 16 rows and 128 columns k; its KS wavefronts share out the reduction in steps of 32 rows of weights.  Lane (g, m) loads, for n =
-// 32 s + 8 g + q (q = 0 .. 7), the dword of codes of columns k = kb + 8 m .. + 7 and their scale; matrix instruction i takes column i
-// of every lane's eight, i.e. its result row 4 g + v stands for column kb + 32 g + 8 v + i.  In bf16 a conversion gives two columns of
-// one n, and pairs along n are put together by byte permutation: one conversion and one permutation per two weights.
-template <typename T, int KS, bool SLOPE>
+// takes 16 rows and 16 C columns k (C = 2 CB, CB bytes of codes a lane); its KS wavefronts share out the reduction in steps of 32 rows of weights.
+// Lane (g, m) loads, for n = 32 s + 8 g + q (q = 0 .. 7), the codes of columns k = kb + C m .. and their scale; matrix instruction i
+// takes column i of every lane's C, i.e. its result row 4 g + v stands for column kb + (4 g + v) C + i.  In bf16 a conversion gives two columns
+// of one n, and pairs along n are put together by byte permutation: one conversion and one permutation per two weights.
+template <typename T, int CB, int KS, bool SLOPE>
 __global__ __launch_bounds__(KS * kWave) void mx4_rows_transposed_kernel(const T* __restrict__ y, Segments seg, int N, int K, Mx4 W,
                                                                   const T* __restrict__ u, T* __restrict__ out, int32_t* __restrict__ status)
 {
-    constexpr int YV = 8 / Store<T>::kVec;
-    static_assert(KS >= 4, "a thread for every eight results");
-    __shared__ f32x4_t red[KS][8][kWave];
+    constexpr int C = 2 * CB, YV = 8 / Store<T>::kVec;
+    static_assert(KS >= 4 && (CB == 4 || (CB == 1 && sizeof(T) == 4)), "a thread for every C results; a dword of codes, or a byte (float)");
+    __shared__ f32x4_t red[KS][C][kWave];
     report_row_overflow(status, seg.offsets, seg.n, seg.max_rows);
-    const int k_blocks = (K + 127) / 128;
-    const int tile = blockIdx.x / k_blocks, kb = (blockIdx.x - tile * k_blocks) * 128;
+    const int k_blocks = (K + 16 * C - 1) / (16 * C);
+    const int tile = blockIdx.x / k_blocks, kb = (blockIdx.x - tile * k_blocks) * 16 * C;
     int expert, row0, row_end;
     if (!find_tile(seg, 16, tile, expert, row0, row_end)) return;
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     const int m = lane & 15, g = lane >> 4;
     const int r = row0 + m < row_end ? row0 + m : row_end - 1;
-    const int k = kb + m * 8;
+    const int k = kb + m * C;
     const bool on = k < K;
     const size_t first = static_cast<size_t>(expert) * N + g * 8;
     const uint8_t* const wc = W.codes + first * (K / 2) + (on ? k / 2 : 0);
     const uint8_t* const ws = W.scales + first * (K / kMxGroup) + (on ? k / kMxGroup : 0);
     const T* const yr = y + static_cast<size_t>(r) * N + g * 8;
-    f32x4_t acc[8];
+    f32x4_t acc[C];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < C; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     for (int n0 = wave * 32; n0 < N; n0 += KS * 32) {
         uint32_t c[8];
         float s[8];
         u32x4_t yv[YV];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {                           // (columns past the end repeat the first; never stored)
-            c[q] = *reinterpret_cast<const uint32_t*>(wc + static_cast<size_t>(n0 + q) * (K / 2));
+            const uint8_t* const from = wc + static_cast<size_t>(n0 + q) * (K / 2);
+            c[q] = CB == 4 ? *reinterpret_cast<const uint32_t*>(from) : *from;
             s[q] = mx4_scale(ws[static_cast<size_t>(n0 + q) * (K / kMxGroup)]);
         }
 #pragma unroll
@@ -165,35 +166,41 @@ __global__ __launch_bounds__(KS * kWave) void mx4_rows_transposed_kernel(const T
             }
         };
         columns(std::integral_constant<int, 0>{});
-        columns(std::integral_constant<int, 1>{});
-        columns(std::integral_constant<int, 2>{});
-        columns(std::integral_constant<int, 3>{});
+        if constexpr (CB == 4) {
+            columns(std::integral_constant<int, 1>{});
+            columns(std::integral_constant<int, 2>{});
+            columns(std::integral_constant<int, 3>{});
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) red[wave][i][lane] = acc[i];
+    for (int i = 0; i < C; ++i) red[wave][i][lane] = acc[i];
     __syncthreads();
-    // thread (row, column octet): octet 4 g + v of the row's 128 columns
-    const int row = threadIdx.x >> 4, octet = threadIdx.x & 15;
-    const int ko = kb + octet * 8;
+    // thread (row, place): place 4 g + v of the row's 16 C columns
+    const int row = threadIdx.x >> 4, place = threadIdx.x & 15;
+    const int ko = kb + place * C;
     if (row0 + row >= row_end || ko >= K || threadIdx.x >= 256) return;
-    float v[8];
+    float v[C];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int from = (octet >> 2) * 16 + row;
-        v[i] = red[0][i][from][octet & 3];
+    for (int i = 0; i < C; ++i) {
+        const int from = (place >> 2) * 16 + row;
+        v[i] = red[0][i][from][place & 3];
 #pragma unroll
-        for (int w = 1; w < KS; ++w) v[i] += red[w][i][from][octet & 3];
+        for (int w = 1; w < KS; ++w) v[i] += red[w][i][from][place & 3];
     }
     const size_t at = static_cast<size_t>(row0 + row) * K + ko;
     if (SLOPE) {
-        float uf[8];
 #pragma unroll
-        for (int i = 0; i < YV; ++i) Store<T>::unpack(*reinterpret_cast<const u32x4_t*>(u + at + i * Store<T>::kVec), uf + i * Store<T>::kVec);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= gelu_slope<T>(uf[i]);
+        for (int i = 0; i < C; ++i) {
+            if constexpr (sizeof(T) == 2) v[i] *= gelu_slope<T>(bf16_to_float(u[at + i]));
+            else v[i] *= gelu_slope<T>(u[at + i]);
+        }
     }
-    store4(out + at, v);
-    store4(out + at + 4, v + 4);
+    if constexpr (C == 8) {
+        store4(out + at, v);
+        store4(out + at + 4, v + 4);
+    } else {
+        *reinterpret_cast<f32x2_t*>(out + at) = f32x2_t{v[0], v[1]};
+    }
 }
 
 namespace {
@@ -209,8 +216,8 @@ long long tile_bound(const Segments& seg, int BM)
 // The tiles of mx4_tile_kernel: 32 RT rows x 32 WN columns, the reduction in KS shares
 template <int RT_, int WN_, int KS_> struct Tile { static constexpr int RT = RT_, WN = WN_, KS = KS_; };
 struct TileSize { int rows, columns, shares; };
-constexpr int kTiles = 5, kFewTile = 3;
-constexpr TileSize kTile[kTiles] = {{128, 256, 1}, {128, 128, 1}, {64, 128, 1}, {32, 128, 2}, {32, 64, 4}};
+constexpr int kTiles = 6, kFewTile = 3;
+constexpr TileSize kTile[kTiles] = {{128, 256, 1}, {128, 128, 1}, {64, 128, 1}, {32, 128, 2}, {32, 64, 4}, {64, 128, 2}};
 
 // Scales by chunks where all of them at once would leave less than three workgroups per compute unit: 4608 -> 1152 with 256 x 128
 // tiles 103 us instead of 113 and with 128 x 128 92 instead of 103, but with 128 x 64, where they leave three, 104 instead of 93
@@ -235,7 +242,8 @@ void with_tile(int tile, int K, F&& f)
     else if (tile == 1) go(Tile<4, 4, 1>{});
     else if (tile == 2) go(Tile<2, 4, 1>{});
     else if (tile == 3) go(Tile<1, 4, 2>{});
-    else go(Tile<1, 2, 4>{});
+    else if (tile == 4) go(Tile<1, 2, 4>{});
+    else go(Tile<2, 4, 2>{});
 }
 
 // Tiles of BM rows x BN columns, a segment's last row tile half full on average
@@ -260,7 +268,7 @@ bool rows_narrow(const Segments& seg, int N) { return tile_bound(seg, 16) * (N /
 int pick_tile(const Segments& seg, int N, int K)
 {
     if (seg.max_rows <= 4 * seg.n && tile_bound(seg, 16) * (N / 32) <= 12 * kComputeUnits) return -1;
-    constexpr float slow[kTiles] = {1.0f, 1.08f, 1.27f, 2.5f};
+    constexpr float slow[kFewTile + 1] = {1.0f, 1.08f, 1.27f, 2.5f};
     int best = -1;
     float least = 0.f;
     for (int i = 0; i <= kFewTile; ++i) {
@@ -270,6 +278,7 @@ int pick_tile(const Segments& seg, int N, int K)
         if (tiles <= kComputeUnits && kTile[i].columns * kTile[i].shares == 128) cost *= 1.3f;
         if (best < 0 || cost < least) { best = i; least = cost; }
     }
+    if (best == 2 && 4 * tile_count(seg, kTile[best].rows, kTile[best].columns, N) <= 5 * kComputeUnits && tile_lds(5, K, tile_chunks(5, K)) <= kLdsBytes) return 5;
     if (best == kFewTile && tile_count(seg, kTile[best].rows, kTile[best].columns, N) <= kComputeUnits &&
         tile_lds(kFewTile + 1, K, tile_chunks(kFewTile + 1, K)) <= kLdsBytes)
         ++best;
@@ -291,7 +300,7 @@ int pick_tile_t(const Segments& seg, int K)
     if (seg.max_rows <= 4 * seg.n && tile_bound(seg, 16) * (K / 128) <= 12 * kComputeUnits) return -1;
     const long long large = tile_count(seg, 64, 256, K), small = tile_count(seg, 32, 128, K);
     if (tile_cost(large, 64, 256) * (large <= kComputeUnits ? 1.3f : 1.0f) <= 1.6f * tile_cost(small, 32, 128)) return 0;
-    return small <= kComputeUnits ? 2 : 1;
+    return 4 * small <= 5 * kComputeUnits ? 2 : 1;
 }
 
 template <typename Shape>
@@ -352,15 +361,20 @@ void transposed_product(const void* y, const Segments& seg, int N, int K, const 
             return;
         }
     }
-    // Eight shares where each has three steps of 32 at least (float, 1000 rows: 1536 -> 384 33 us against 54 with four; 384 -> 1536 31 against 25)
-    auto go = [&](auto shares) {
-        constexpr int KS = decltype(shares)::value;
-        const long long blocks = tile_bound(seg, 16) * ((K + 127) / 128);
-        hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream,
+    // Eight shares where each has three steps of 32 at least (float, 1000 rows: 1536 -> 384 33 us against 54 with four; 384 -> 1536 31 against
+    // 25).  Float, whose matrix instructions take an eighth of the rate: 32 columns and sixteen shares where 128 columns leave half of the
+    // compute units empty (two rows, 1152 -> 4608 17 us against 27, 4608 -> 1152 40 against 86; bf16 12 against 7 and 12 against 13).
+    auto go = [&](auto bytes, auto shares) {
+        constexpr int CB = decltype(bytes)::value, KS = decltype(shares)::value;
+        const long long blocks = tile_bound(seg, 16) * ((K + 32 * CB - 1) / (32 * CB));
+        hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, CB, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream,
                            static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
     };
-    if (N >= 768) go(std::integral_constant<int, 8>{});
-    else go(std::integral_constant<int, 4>{});
+    if constexpr (sizeof(T) == 4) {
+        if (2 * tile_bound(seg, 16) * ((K + 127) / 128) <= kComputeUnits) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
+    }
+    if (N >= 768) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
+    else go(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
 }
 
 template <typename T>
@@ -392,6 +406,7 @@ hipError_t prepare_expert_ffn_mx4()
     if (err == hipSuccess) err = configure_tile<Tile<2, 4, 1>>();
     if (err == hipSuccess) err = configure_tile<Tile<1, 4, 2>>();
     if (err == hipSuccess) err = configure_tile<Tile<1, 2, 4>>();
+    if (err == hipSuccess) err = configure_tile<Tile<2, 4, 2>>();
     const auto shares = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<1, 2, 4, false>);
     const auto shares_slope = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<1, 2, 4, true>);
     for (const void* kernel : {shares, shares_slope})            // (the other transposed tiles need less than the 64 KiB that every kernel has)
