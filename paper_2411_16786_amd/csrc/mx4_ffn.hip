@@ -7,6 +7,7 @@
 #include "ffn_mfma.hpp"
 #include "kernels.hpp"
 #include "mx4.hpp"
+#include "mx4_plan.hpp"
 #include "mx4_tile.hpp"
 #include "mx4_tile_t.hpp"
 
@@ -205,29 +206,8 @@ __global__ __launch_bounds__(KS * kWave) void mx4_rows_transposed_kernel(const T
 
 namespace {
 
-// most row tiles of BM rows that a table of n segments with max_rows rows can have (one at least: a block reports the row count)
-long long tile_bound(const Segments& seg, int BM)
-{
-    const long long most = static_cast<long long>(seg.max_rows) / BM + seg.n;       // every segment may end in a part of a tile
-    const long long tiles = most < seg.max_rows ? most : seg.max_rows;              // ... and a tile has a row at least
-    return tiles > 1 ? tiles : 1;
-}
-
-// The tiles of mx4_tile_kernel: 32 RT rows x 32 WN columns, the reduction in KS shares
+// A tile as its kernel takes it: 32 RT rows, 32 WN columns (64 WN in the transposed kernel), the reduction in KS shares
 template <int RT_, int WN_, int KS_> struct Tile { static constexpr int RT = RT_, WN = WN_, KS = KS_; };
-struct TileSize { int rows, columns, shares; };
-constexpr int kTiles = 6, kFewTile = 3;
-constexpr TileSize kTile[kTiles] = {{128, 256, 1}, {128, 128, 1}, {64, 128, 1}, {32, 128, 2}, {32, 64, 4}, {64, 128, 2}};
-
-// Scales by chunks where all of them at once would leave less than three workgroups per compute unit: 4608 -> 1152 with 256 x 128
-// tiles 103 us instead of 113 and with 128 x 128 92 instead of 103, but with 128 x 64, where they leave three, 104 instead of 93
-int tile_lds(int tile, int K, bool chunks)
-{
-    const TileSize t = kTile[tile];
-    const int unit = 32 * t.columns * t.shares;                  // a workgroup's 16-byte loads
-    return t.shares * (2 * t.rows * 128 + 2 * t.columns * 64 + (chunks ? 2 * t.columns * 16 : 0)) + (chunks ? 0 : (t.columns / 32 * K + unit - 1) / unit * unit);
-}
-bool tile_chunks(int tile, int K) { return K % 512 == 0 && 3 * tile_lds(tile, K, false) > kLdsBytes; }
 
 // Calls f with the shape of a tile and whether its scales go by chunks
 template <typename F>
@@ -246,48 +226,6 @@ void with_tile(int tile, int K, F&& f)
     else go(Tile<2, 4, 2>{});
 }
 
-// Tiles of BM rows x BN columns, a segment's last row tile half full on average
-long long tile_count(const Segments& seg, int BM, int BN, int columns)
-{
-    const long long row_tiles = (seg.max_rows + seg.n * BM / 2) / BM;
-    return (row_tiles > seg.n ? row_tiles : seg.n) * ((columns + BN - 1) / BN);
-}
-// ... and by area what the compute unit with the most of them has to do
-float tile_cost(long long tiles, int BM, int BN) { return static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (BM * BN); }
-
-// Columns per wavefront set of mx4_rows_kernel: 16 while that gives each compute unit no more than six workgroups (4608 -> 1152, one token
-// 6.6 us against 9.6 with 32, eight tokens 9.1 and 10.0), else 32 (1152 -> 4608, eight tokens 9.2 against 11.6)
-bool rows_narrow(const Segments& seg, int N) { return tile_bound(seg, 16) * (N / 16) <= 6 * kComputeUnits; }
-
-// Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel), which up to four rows a segment is faster while it has at
-// most 12 workgroups per compute unit (eight tokens at the DiT-MoE-XL widths 9.2 and 9.1 us against 11.5 and 13.0; 26 rows over 16
-// experts, 2048 -> 8192, 27.8 against 22.6).  Among the tiles that with their scales fit the LDS the cheapest by area, at the
-// rates of 8192 -> 4096 of 8192 rows (444, 481 and 563 us; the tiles of 32 rows are for few rows); a compute unit with a single workgroup
-// of four wavefronts waits more.  Of the two of 32 rows, in shares, the narrower one in more shares while each tile has a compute unit
-// to itself (200 rows over 8 experts: 4608 -> 1152 13.4 us against 21.8, 1152 -> 4608, 288 tiles, 16.6 against 12.6).
-int pick_tile(const Segments& seg, int N, int K)
-{
-    if (seg.max_rows <= 4 * seg.n && tile_bound(seg, 16) * (N / 32) <= 12 * kComputeUnits) return -1;
-    constexpr float slow[kFewTile + 1] = {1.0f, 1.08f, 1.27f, 2.5f};
-    int best = -1;
-    float least = 0.f;
-    for (int i = 0; i <= kFewTile; ++i) {
-        if (tile_lds(i, K, tile_chunks(i, K)) > kLdsBytes) continue;
-        const long long tiles = tile_count(seg, kTile[i].rows, kTile[i].columns, N);
-        float cost = slow[i] * tile_cost(tiles, kTile[i].rows, kTile[i].columns);
-        if (tiles <= kComputeUnits && kTile[i].columns * kTile[i].shares == 128) cost *= 1.3f;
-        if (best < 0 || cost < least) { best = i; least = cost; }
-    }
-    if (best == 2 && 4 * tile_count(seg, kTile[best].rows, kTile[best].columns, N) <= 5 * kComputeUnits && tile_lds(5, K, tile_chunks(5, K)) <= kLdsBytes) return 5;
-    if (best == kFewTile && tile_count(seg, kTile[best].rows, kTile[best].columns, N) <= kComputeUnits &&
-        tile_lds(kFewTile + 1, K, tile_chunks(kFewTile + 1, K)) <= kLdsBytes)
-        ++best;
-    return best;
-}
-
-// The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns of K; its LDS does not depend on the reduction).  4608 -> 1152, 8192
-// rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23.  1152 -> 4608,
-// 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
 template <typename F>
 void with_tile_t(int tile, F&& f)
 {
@@ -295,14 +233,6 @@ void with_tile_t(int tile, F&& f)
     else if (tile == 1) f(Tile<1, 2, 2>{});
     else f(Tile<1, 2, 4>{});
 }
-int pick_tile_t(const Segments& seg, int K)
-{
-    if (seg.max_rows <= 4 * seg.n && tile_bound(seg, 16) * (K / 128) <= 12 * kComputeUnits) return -1;
-    const long long large = tile_count(seg, 64, 256, K), small = tile_count(seg, 32, 128, K);
-    if (tile_cost(large, 64, 256) * (large <= kComputeUnits ? 1.3f : 1.0f) <= 1.6f * tile_cost(small, 32, 128)) return 0;
-    return 4 * small <= 5 * kComputeUnits ? 2 : 1;
-}
-
 template <typename Shape>
 hipError_t configure_tile()
 {
@@ -320,13 +250,13 @@ void rows_product(const void* x, const int32_t* row_index, int row_div, const Se
                   void* pre, void* out, const int32_t* out_index, int32_t* status, hipStream_t stream)
 {
     if constexpr (sizeof(T) == 2) {
-        const int tile = pick_tile(seg, N, K);
+        const int tile = pick_tile(seg.max_rows, seg.n, N, K);
         if (tile >= 0) {
             with_tile(tile, K, [&](auto shape, auto chunks) {
                 constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN, KS = decltype(shape)::KS;
                 constexpr bool CHUNKS = decltype(chunks)::value;
                 typedef TileShape<RT, WN, KS, CHUNKS> S;
-                const long long blocks = (tile_bound(seg, S::BR) * ((N + S::BN - 1) / S::BN) + 7) / 8 * 8;
+                const long long blocks = (tile_bound(seg.max_rows, seg.n, S::BR) * ((N + S::BN - 1) / S::BN) + 7) / 8 * 8;
                 hipLaunchKernelGGL((mx4_tile_kernel<RT, WN, KS, CHUNKS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * S::kThreads), S::lds_bytes(K),
                                    stream, static_cast<const T*>(x), row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out),
                                    out_index, status);
@@ -336,11 +266,11 @@ void rows_product(const void* x, const int32_t* row_index, int row_div, const Se
     }
     auto go = [&](auto narrow) {
         constexpr int NT = decltype(narrow)::value ? 1 : 2, KS = 8;
-        const long long blocks = tile_bound(seg, 16) * ((N + 16 * NT - 1) / (16 * NT));
+        const long long blocks = tile_bound(seg.max_rows, seg.n, 16) * ((N + 16 * NT - 1) / (16 * NT));
         hipLaunchKernelGGL((mx4_rows_kernel<T, NT, KS, GELU>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream, static_cast<const T*>(x),
                            row_index, row_div, seg, N, K, W, bias, static_cast<T*>(pre), static_cast<T*>(out), out_index, status);
     };
-    if (rows_narrow(seg, N)) go(std::true_type{});
+    if (rows_narrow(seg.max_rows, seg.n, N)) go(std::true_type{});
     else go(std::false_type{});
 }
 
@@ -348,13 +278,13 @@ template <typename T, bool SLOPE>
 void transposed_product(const void* y, const Segments& seg, int N, int K, const Mx4& W, const void* u, void* out, int32_t* status, hipStream_t stream)
 {
     if constexpr (sizeof(T) == 2) {
-        const int tile = pick_tile_t(seg, K);
+        const int tile = pick_tile_t(seg.max_rows, seg.n, K);
         if (tile >= 0) {
             with_tile_t(tile, [&](auto shape) {
                 constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN, KS = decltype(shape)::KS;
                 typedef TileShapeT<RT, WN, KS> S;
                 static_assert(KS == 4 || S::kLds <= 64 * 1024, "no raised limit");
-                const long long blocks = (tile_bound(seg, S::BR) * ((K + S::BK - 1) / S::BK) + 7) / 8 * 8;
+                const long long blocks = (tile_bound(seg.max_rows, seg.n, S::BR) * ((K + S::BK - 1) / S::BK) + 7) / 8 * 8;
                 hipLaunchKernelGGL((mx4_tile_transposed_kernel<RT, WN, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * S::kThreads), S::kLds, stream,
                                    static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
             });
@@ -366,12 +296,12 @@ void transposed_product(const void* y, const Segments& seg, int N, int K, const 
     // compute units empty (two rows, 1152 -> 4608 17 us against 27, 4608 -> 1152 40 against 86; bf16 12 against 7 and 12 against 13).
     auto go = [&](auto bytes, auto shares) {
         constexpr int CB = decltype(bytes)::value, KS = decltype(shares)::value;
-        const long long blocks = tile_bound(seg, 16) * ((K + 32 * CB - 1) / (32 * CB));
+        const long long blocks = tile_bound(seg.max_rows, seg.n, 16) * ((K + 32 * CB - 1) / (32 * CB));
         hipLaunchKernelGGL((mx4_rows_transposed_kernel<T, CB, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * kWave), 0, stream,
                            static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
     };
     if constexpr (sizeof(T) == 4) {
-        if (2 * tile_bound(seg, 16) * ((K + 127) / 128) <= kComputeUnits) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
+        if (2 * tile_bound(seg.max_rows, seg.n, 16) * ((K + 127) / 128) <= kComputeUnits) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
     }
     if (N >= 768) go(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
     else go(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});

@@ -1,0 +1,83 @@
+// Which kernel and tile the 4-bit expert FFN takes (mx4_ffn.hip), from sizes that the host knows: plain C++.
+#pragma once
+#include "ffn_plan.hpp"
+
+namespace dicemoe {
+
+constexpr int kLdsBytes = 160 * 1024;
+
+// most row tiles of BM rows that a table of n segments with max_rows rows can have (one at least: a block reports the row count)
+inline long long tile_bound(int max_rows, int n_seg, int BM)
+{
+    const long long most = static_cast<long long>(max_rows) / BM + n_seg;       // every segment may end in a part of a tile
+    const long long tiles = most < max_rows ? most : max_rows;              // ... and a tile has a row at least
+    return tiles > 1 ? tiles : 1;
+}
+
+// The tiles of mx4_tile_kernel: rows, columns, shares of the reduction; the first four are weighed against each other, the others take the place of
+// one of them where few tiles leave compute units empty
+struct TileSize { int rows, columns, shares; };
+constexpr int kTiles = 6, kFewTile = 3;
+constexpr TileSize kTile[kTiles] = {{128, 256, 1}, {128, 128, 1}, {64, 128, 1}, {32, 128, 2}, {32, 64, 4}, {64, 128, 2}};
+
+// Scales by chunks where all of them at once would leave less than three workgroups per compute unit: 4608 -> 1152 with 256 x 128
+// tiles 103 us instead of 113 and with 128 x 128 92 instead of 103, but with 128 x 64, where they leave three, 104 instead of 93
+inline int tile_lds(int tile, int K, bool chunks)
+{
+    const TileSize t = kTile[tile];
+    const int unit = 32 * t.columns * t.shares;                  // a workgroup's 16-byte loads
+    return t.shares * (2 * t.rows * 128 + 2 * t.columns * 64 + (chunks ? 2 * t.columns * 16 : 0)) + (chunks ? 0 : (t.columns / 32 * K + unit - 1) / unit * unit);
+}
+inline bool tile_chunks(int tile, int K) { return K % 512 == 0 && 3 * tile_lds(tile, K, false) > kLdsBytes; }
+
+// Tiles of BM rows x BN columns, a segment's last row tile half full on average
+inline long long tile_count(int max_rows, int n_seg, int BM, int BN, int columns)
+{
+    const long long row_tiles = (max_rows + n_seg * BM / 2) / BM;
+    return (row_tiles > n_seg ? row_tiles : n_seg) * ((columns + BN - 1) / BN);
+}
+// ... and by area what the compute unit with the most of them has to do
+inline float tile_cost(long long tiles, int BM, int BN) { return static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (BM * BN); }
+
+// Columns per wavefront set of mx4_rows_kernel: 16 while that gives each compute unit no more than six workgroups (4608 -> 1152, one token
+// 6.6 us against 9.6 with 32, eight tokens 9.1 and 10.0), else 32 (1152 -> 4608, eight tokens 9.2 against 11.6)
+inline bool rows_narrow(int max_rows, int n_seg, int N) { return tile_bound(max_rows, n_seg, 16) * (N / 16) <= 6 * kComputeUnits; }
+
+// Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel), which up to four rows a segment is faster while it has at
+// most 12 workgroups per compute unit (eight tokens at the DiT-MoE-XL widths 9.2 and 9.1 us against 11.5 and 13.0; 26 rows over 16
+// experts, 2048 -> 8192, 27.8 against 22.6).  Among the tiles that with their scales fit the LDS the cheapest by area, at the
+// rates of 8192 -> 4096 of 8192 rows (444, 481 and 563 us; the tiles of 32 rows are for few rows); a compute unit with a single workgroup
+// of four wavefronts waits more.  Of the two of 32 rows, in shares, the narrower one in more shares while each tile has a compute unit
+// to itself (200 rows over 8 experts: 4608 -> 1152 13.4 us against 21.8, 1152 -> 4608, 288 tiles, 16.6 against 12.6).
+inline int pick_tile(int max_rows, int n_seg, int N, int K)
+{
+    if (max_rows <= 4 * n_seg && tile_bound(max_rows, n_seg, 16) * (N / 32) <= 12 * kComputeUnits) return -1;
+    constexpr float slow[kFewTile + 1] = {1.0f, 1.08f, 1.27f, 2.5f};
+    int best = -1;
+    float least = 0.f;
+    for (int i = 0; i <= kFewTile; ++i) {
+        if (tile_lds(i, K, tile_chunks(i, K)) > kLdsBytes) continue;
+        const long long tiles = tile_count(max_rows, n_seg, kTile[i].rows, kTile[i].columns, N);
+        float cost = slow[i] * tile_cost(tiles, kTile[i].rows, kTile[i].columns);
+        if (tiles <= kComputeUnits && kTile[i].columns * kTile[i].shares == 128) cost *= 1.3f;
+        if (best < 0 || cost < least) { best = i; least = cost; }
+    }
+    if (best == 2 && 4 * tile_count(max_rows, n_seg, kTile[best].rows, kTile[best].columns, N) <= 5 * kComputeUnits && tile_lds(5, K, tile_chunks(5, K)) <= kLdsBytes) return 5;
+    if (best == kFewTile && tile_count(max_rows, n_seg, kTile[best].rows, kTile[best].columns, N) <= kComputeUnits &&
+        tile_lds(kFewTile + 1, K, tile_chunks(kFewTile + 1, K)) <= kLdsBytes)
+        ++best;
+    return best;
+}
+
+// The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns of K; its LDS does not depend on the reduction).  4608 -> 1152, 8192
+// rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23.  1152 -> 4608,
+// 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
+inline int pick_tile_t(int max_rows, int n_seg, int K)
+{
+    if (max_rows <= 4 * n_seg && tile_bound(max_rows, n_seg, 16) * (K / 128) <= 12 * kComputeUnits) return -1;
+    const long long large = tile_count(max_rows, n_seg, 64, 256, K), small = tile_count(max_rows, n_seg, 32, 128, K);
+    if (tile_cost(large, 64, 256) * (large <= kComputeUnits ? 1.3f : 1.0f) <= 1.6f * tile_cost(small, 32, 128)) return 0;
+    return 4 * small <= 5 * kComputeUnits ? 2 : 1;
+}
+
+}  // namespace dicemoe

@@ -113,7 +113,6 @@ __device__ __forceinline__ bool find_tile_on_xcd(const Segments& s, int BM, int 
 
 // BN columns, BR rows.  CHUNKS: scales in chunks of 512 reduction columns (16 bytes a row, two chunks in the LDS; K % 512 == 0) instead
 // of all of them at once (rows of weights are adjacent in memory, so is what is staged).
-constexpr int kLdsBytes = 160 * 1024;
 template <int RT, int WN, int KS, bool CHUNKS> struct TileShape {
     static constexpr int BN = 32 * WN, BR = 32 * RT, kThreads = 64 * WN;            // (of one share)
     static constexpr int kRowBytes = BR * 128, kCodeBytes = BN * 64;           // of a stage, of a pair of stages
