@@ -233,6 +233,7 @@ void with_tile_t(int tile, F&& f)
     else if (tile == 1) f(Tile<1, 2, 2>{});
     else f(Tile<1, 2, 4>{});
 }
+
 template <typename Shape>
 hipError_t configure_tile()
 {

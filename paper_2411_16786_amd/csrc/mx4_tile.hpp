@@ -39,7 +39,8 @@ template <> __device__ __forceinline__ float mx4_gelu<bf16_t>(float u) { return 
 // gelu'(u) = Phi(u) + u phi(u); with a = |u| it is 1 - s for u >= 0 and s below, s = Phi(-a) - a phi(a)
 template <typename T> __device__ __forceinline__ float gelu_slope(float u);
 template <> __device__ __forceinline__ float gelu_slope<float>(float u) {
-    return 0.5f * (1.0f + erff(u * 0.70710678118654752440f)) + u * (0.39894228040143267794f * expf(-0.5f * u * u));
+    const float a = fminf(fabsf(u), 40.0f);                     // (infinity times the bell's zero is no number; u phi(u) is zero from 15 on)
+    return 0.5f * (1.0f + erff(u * 0.70710678118654752440f)) + copysignf(a, u) * (0.39894228040143267794f * expf(-0.5f * a * a));
 }
 template <> __device__ __forceinline__ float gelu_slope<bf16_t>(float u) {
     const float a = fminf(fabsf(u), 6.0f);

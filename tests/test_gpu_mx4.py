@@ -315,6 +315,22 @@ def test_values_that_are_not_finite_stay_in_their_rows(dtype, T):
     assert torch.isnan(du[3, 7]) and torch.isnan(dx[3].float()).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [5, 300])
+def test_slope_of_infinite_and_large_pre_activations(dtype, T):
+    """gelu' is 1 at +infinity and 0 at -infinity; far out it is within the forms' 4e-6 of that."""
+    c = Case(T, 128, 256, 1, 1, dtype)
+    ends = torch.tensor([float("inf"), -float("inf"), 1e30, -1e30, 60.0, -60.0, 7.0, -7.0])
+    u = ends[torch.randint(0, 8, (T, 256), generator=c.gen)].to(c.dt)
+    dh = torch.randn((T, 128), generator=c.gen).to(c.dt)
+    du, dx = c.backward(dh.cuda(), u.cuda())
+    raw, tol = M.times_weights(dh.double(), c.offsets, range(1), c.v2, "f32")
+    want = raw * (u > 0)
+    off = tol + 4e-6 * (raw.abs() + tol)
+    M.within(du, want, off + M.HALF[dtype] * (want.abs() + off), "du")
+    assert torch.isfinite(dx.float()).all()
+
+
 def test_scale_byte_255_is_nan_and_its_column_alone():
     c = Case(6, 128, 256, 2, 1, "bf16")
     u, _ = c.forward()
