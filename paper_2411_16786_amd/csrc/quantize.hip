@@ -59,19 +59,29 @@ __global__ __launch_bounds__(256) void quantize_mx4_kernel(const T* __restrict__
     }
 }
 
+namespace {
+
+template <typename T>
+hipError_t launch_quantize_mx4_t(const T* W, long long octets, uint8_t* codes, uint8_t* scales, T* values, hipStream_t stream)
+{
+    constexpr long long kMost = 1ll << 30;                      // octets per launch: a grid holds less than 2^32 threads
+    for (long long o = 0; o < octets; o += kMost) {
+        const long long n = octets - o < kMost ? octets - o : kMost;
+        hipLaunchKernelGGL(quantize_mx4_kernel<T>, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, W + o * 8, n, codes + o * 4,
+                           scales + o / 4, values ? values + o * 8 : nullptr);
+        if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
 hipError_t launch_quantize_mx4(bool bf16, const void* W, long long rows, int cols, uint8_t* codes, uint8_t* scales, void* values,
                                hipStream_t stream)
 {
     const long long octets = rows * (cols / 8);
-    if (octets == 0) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>((octets + 255) / 256));
-    if (bf16)
-        hipLaunchKernelGGL(quantize_mx4_kernel<bf16_t>, grid, dim3(256), 0, stream, static_cast<const bf16_t*>(W), octets, codes, scales,
-                           static_cast<bf16_t*>(values));
-    else
-        hipLaunchKernelGGL(quantize_mx4_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float*>(W), octets, codes, scales,
-                           static_cast<float*>(values));
-    return hipGetLastError();
+    if (bf16) return launch_quantize_mx4_t(static_cast<const bf16_t*>(W), octets, codes, scales, static_cast<bf16_t*>(values), stream);
+    return launch_quantize_mx4_t(static_cast<const float*>(W), octets, codes, scales, static_cast<float*>(values), stream);
 }
 
 }  // namespace dicemoe

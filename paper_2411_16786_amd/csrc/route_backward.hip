@@ -69,7 +69,9 @@ __global__ __launch_bounds__(256) void route_logits_kernel(RouteBackward a)
     if (a.renorm) {
         total = 0.f;
         for (int j = 0; j < a.k; ++j) {
-            const float p = a.probs[te + a.idx[tk + j]];
+            const int e = a.idx[tk + j];
+            if (e < 0 || e >= a.E) continue;             // (no expert of this router: no part in the sum)
+            const float p = a.probs[te + e];
             total += p;
             mean = fmaf(a.dscores[tk + j], p, mean);
         }

@@ -104,6 +104,26 @@ def test_quantize_marks_groups_that_are_not_finite(dtype):
     assert (codes.cpu().reshape(4, 3, 16)[bad] == 0).all()
 
 
+def test_quantize_beyond_32_bit_offsets():
+    """2^33 weights and some: more than one launch, offsets beyond 32 bits; every piece as the call on it alone gives it."""
+    ctx = B.Context(1, 64, 64, 1, 1, "bf16")
+    rows, cols = (1 << 20) + 3, 8192
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    W = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    places = [0, 1, (1 << 18) - 1, 1 << 18, (1 << 19) + 5, (1 << 20) - 1, 1 << 20, rows - 1]        # 2^32 bytes and 2^33 elements among them
+    W[places] = torch.randn((len(places), cols), generator=gen, device="cuda").bfloat16()
+    codes = torch.full((rows, cols // 2), 171, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, cols // 32), 171, dtype=torch.uint8, device="cuda")
+    ctx.moe_quantize_mx4(W, codes, scales)
+    few = W[places].contiguous()
+    few_codes, few_scales = torch.empty_like(codes[:len(places)]), torch.empty_like(scales[:len(places)])
+    ctx.moe_quantize_mx4(few, few_codes, few_scales)
+    torch.cuda.synchronize()
+    assert torch.equal(codes[places], few_codes) and torch.equal(scales[places], few_scales)
+    codes[places], scales[places] = 0, 1
+    assert int(codes.amax()) == 0 and int(scales.amax()) == 1 and int(scales.amin()) == 1
+
+
 # ---- the FFN and its gradient
 
 class Case:
