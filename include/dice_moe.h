@@ -363,7 +363,7 @@ int moe_quantize_mx4(moe_ctx* ctx, const void* W, int64_t rows, int32_t cols, ui
  *        seg_offsets, seg_expert, n_segments, max_rows, b1, b2 as in moe_expert_ffn.  Packed rows from max_rows on are not
  *        touched (moe_expert_ffn_status reports that there were some), nor are segments whose expert is out of range
  *   out: h_rows (dtype); u_packed[..][F] (dtype, may be NULL): the pre-activations by packed row, for the gradient
- * workspace: moe_workspace_bytes().  d and F multiples of 32, at most 2^20. */
+ * workspace: moe_workspace_bytes().  d and F multiples of 32, at most 2^20; min(max_rows, max_rows / 16 + n_segments) * max(d, F) < 2^28. */
 int moe_expert_ffn_mx4(moe_ctx* ctx, const void* x_rows, const int32_t* row_pairs, const int32_t* out_pairs,
                        const int32_t* seg_offsets, const int32_t* seg_expert, int32_t n_segments, int32_t max_rows,
                        const uint8_t* W1_codes, const uint8_t* W1_scales, const float* b1, const uint8_t* W2_codes,

@@ -188,13 +188,18 @@ int check_ffn(moe_ctx* ctx, const char* who, const void* x_rows, const int32_t* 
     return MOE_OK;
 }
 
-// The 4-bit expert FFN calls: whole scale groups in every weight row, offsets inside one expert's codes well within 64 bits, and a
-// launch of at most 2^31 workgroups
-int check_mx4(moe_ctx* ctx, const char* who)
+// The 4-bit expert FFN calls: whole scale groups in every weight row, offsets inside one expert's codes well within 64 bits, and less
+// than the 2^32 threads that a launch holds (the kernels of few rows have most: 512 for 16 rows and 32 columns)
+int check_mx4(moe_ctx* ctx, const char* who, int32_t n_segments, int32_t max_rows)
 {
     const moe_shape& s = ctx->shape;
     if (s.d % 32 != 0 || s.F % 32 != 0 || s.d > (1 << 20) || s.F > (1 << 20)) {
         std::snprintf(ctx->err, sizeof(ctx->err), "%s: d=%d and F=%d have to be multiples of 32 up to 2^20", who, s.d, s.F);
+        return MOE_ERR_SHAPE;
+    }
+    const long long tiles = max_rows < max_rows / 16ll + n_segments ? max_rows : max_rows / 16ll + n_segments;
+    if (tiles * (s.d > s.F ? s.d : s.F) >= 1ll << 28) {
+        std::snprintf(ctx->err, sizeof(ctx->err), "%s: max_rows=%d in n_segments=%d are too many at these widths", who, max_rows, n_segments);
         return MOE_ERR_SHAPE;
     }
     return MOE_OK;
@@ -574,7 +579,7 @@ int moe_expert_ffn_mx4(moe_ctx* ctx, const void* x_rows, const int32_t* row_pair
 {
     const char* const who = "moe_expert_ffn_mx4";
     if (!ctx) return MOE_ERR_NULL;
-    if (int rc = check_mx4(ctx, who)) return rc;
+    if (int rc = check_mx4(ctx, who, n_segments, max_rows)) return rc;
     if (max_rows == 0) x_rows = h_rows = workspace;      // no row is read or written: an empty tensor's null will do
     if (int rc = check_ffn(ctx, who, x_rows, seg_offsets, seg_expert, n_segments, max_rows, W1_codes, W2_codes, h_rows, workspace)) return rc;
     if (!W1_scales || !W2_scales) return fail(ctx, MOE_ERR_NULL, "moe_expert_ffn_mx4: scales are null");
@@ -595,7 +600,7 @@ int moe_expert_ffn_mx4_backward(moe_ctx* ctx, const void* dh_packed, const void*
 {
     const char* const who = "moe_expert_ffn_mx4_backward";
     if (!ctx) return MOE_ERR_NULL;
-    if (int rc = check_mx4(ctx, who)) return rc;
+    if (int rc = check_mx4(ctx, who, n_segments, max_rows)) return rc;
     if (max_rows == 0) dh_packed = u_packed = dx_packed = workspace;
     if (int rc = check_ffn(ctx, who, dh_packed, seg_offsets, seg_expert, n_segments, max_rows, W1_codes, W2_codes, dx_packed, workspace)) return rc;
     if (!u_packed || !W1_scales || !W2_scales) return fail(ctx, MOE_ERR_NULL, "moe_expert_ffn_mx4_backward: null pointer");

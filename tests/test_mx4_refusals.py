@@ -54,6 +54,8 @@ def test_ffn_calls_refuse(call, required):
     assert call(_ctx(d=48, dtype="f32")) == B.MOE_ERR_SHAPE
     assert call(_ctx(F=240, dtype="f32")) == B.MOE_ERR_SHAPE
     assert call(_ctx(T_max=1, F=1 << 21)) == B.MOE_ERR_SHAPE
+    # a table of so many short segments that a launch would have 2^32 threads
+    assert call(_ctx(T_max=512, d=64, F=1 << 20), max_rows=512, n_seg=512) == B.MOE_ERR_SHAPE
 
 
 def test_combine_backward_refuses():
