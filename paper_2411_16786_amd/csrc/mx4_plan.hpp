@@ -43,6 +43,11 @@ inline float tile_cost(long long tiles, int BM, int BN) { return static_cast<flo
 // 6.6 us against 9.6 with 32, eight tokens 9.1 and 10.0), else 32 (1152 -> 4608, eight tokens 9.2 against 11.6)
 inline bool rows_narrow(int max_rows, int n_seg, int N) { return tile_bound(max_rows, n_seg, 16) * (N / 16) <= 6 * kComputeUnits; }
 
+// Float rows, which have no tiles: 64 columns and four shares instead of eight where that leaves each compute unit more than four
+// workgroups (1000 rows over 16 experts, 384 -> 1536 24 us against 31; 2000 over 8, 4608 -> 1152 224 against 252; with 468 workgroups,
+// 300 rows over 8, 4608 -> 1152 57 against 55)
+inline bool rows_wide(int max_rows, int n_seg, int N) { return tile_bound(max_rows, n_seg, 16) * ((N + 63) / 64) > 4 * kComputeUnits; }
+
 // Tile of a product of many rows, -1: rows in sixteens (mx4_rows_kernel), which up to four rows a segment is faster while it has at
 // most 12 workgroups per compute unit (eight tokens at the DiT-MoE-XL widths 9.2 and 9.1 us against 11.5 and 13.0; 26 rows over 16
 // experts, 2048 -> 8192, 27.8 against 22.6).  Among the tiles that with their scales fit the LDS the cheapest by area, at the

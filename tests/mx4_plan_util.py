@@ -11,6 +11,7 @@ extern "C" int tile(int rows, int n_seg, int N, int K) { return dicemoe::pick_ti
 extern "C" int chunks(int tile, int K) { return dicemoe::tile_chunks(tile, K) ? 1 : 0; }
 extern "C" int lds(int tile, int K) { return dicemoe::tile_lds(tile, K, dicemoe::tile_chunks(tile, K)); }
 extern "C" int narrow(int rows, int n_seg, int N) { return dicemoe::rows_narrow(rows, n_seg, N) ? 1 : 0; }
+extern "C" int wide(int rows, int n_seg, int N) { return dicemoe::rows_wide(rows, n_seg, N) ? 1 : 0; }
 extern "C" int tile_t(int rows, int n_seg, int K) { return dicemoe::pick_tile_t(rows, n_seg, K); }
 extern "C" long long bound(int rows, int n_seg, int BM) { return dicemoe::tile_bound(rows, n_seg, BM); }
 """
@@ -36,6 +37,10 @@ def plan(rows, n_seg, N, K):
     if t < 0:
         return "rows16" if lib().narrow(rows, n_seg, N) else "rows32"
     return TILES[t] + ("+" if lib().chunks(t, K) else "")
+
+
+def plan_float(rows, n_seg, N):
+    return "rows64" if lib().wide(rows, n_seg, N) else "rows16" if lib().narrow(rows, n_seg, N) else "rows32"
 
 
 def plan_t(rows, n_seg, K):

@@ -218,6 +218,8 @@ CASES = [
     (64, 64, 256, 4, 2, "f32", True, 0.0, None),
     (200, 384, 1536, 16, 2, "f32", True, 0.0, None),
     (333, 224, 288, 3, 3, "f32", True, 0.1, [0, 1, 2]),
+    (500, 384, 1536, 16, 2, "f32", True, 0.1, None),                 # 64 columns a workgroup in the first product
+    (1300, 1056, 288, 2, 1, "f32", True, 0.0, None),                 # ... in the second, whose last 64 are half there
 ]
 
 

@@ -36,3 +36,13 @@ def test_tile_bound(rows, n_seg, BM, tiles):
 ])
 def test_choices(rows, n_seg, d, F, names):
     assert P.plans(rows, n_seg, d, F) == names
+
+
+@pytest.mark.parametrize("rows,n_seg,d,F,names", [
+    (2, 8, 1152, 4608, ("rows16", "rows16")),
+    (120, 16, 384, 1536, ("rows32", "rows16")),
+    (1000, 16, 384, 1536, ("rows64", "rows32")),
+    (2000, 8, 1152, 4608, ("rows64", "rows64")),
+])
+def test_choices_in_float(rows, n_seg, d, F, names):
+    assert (P.plan_float(rows, n_seg, F), P.plan_float(rows, n_seg, d)) == names
