@@ -330,9 +330,10 @@ void transposed_product(const void* y, const Segments& seg, int N, int K, const 
             return;
         }
     }
-    // Eight shares where each has three steps of 32 at least (float, 1000 rows: 1536 -> 384 33 us against 54 with four; 384 -> 1536 31 against
-    // 25).  Float, whose matrix instructions take an eighth of the rate: 32 columns and sixteen shares where 128 columns leave half of the
-    // compute units empty (two rows, 1152 -> 4608 17 us against 27, 4608 -> 1152 40 against 86; bf16 12 against 7 and 12 against 13).
+    // Eight shares where each has three steps of 32 at least (two rows in bf16: 4608 -> 1152 13.8 us against 20.8 with four, 1536 -> 384 7.5
+    // and 8.8; float, 1000 rows, 384 -> 1536 29 against 25).  Float, whose matrix instructions take an eighth of the rate: 32 columns and
+    // sixteen shares where 128 columns leave half of the compute units empty (two rows, 4608 -> 1152 20 us against 47, 1152 -> 4608 17
+    // both; in bf16 12 against 7 and 12 against 13).
     auto go = [&](auto bytes, auto shares) {
         constexpr int CB = decltype(bytes)::value, KS = decltype(shares)::value;
         const long long blocks = tile_bound(seg.max_rows, seg.n, 16) * ((K + 32 * CB - 1) / (32 * CB));

@@ -102,12 +102,12 @@ __global__ __launch_bounds__(256) void route_logits_kernel(RouteBackward a)
 // consecutive columns of tokens 4g .. 4g + 3 in the lane that also gathers the dispatch's rows for them and stores 16 bytes.  dz^T x stays in registers
 // over a wavefront's tiles; the four meet in LDS in wavefront order, and workgroups write partial sums [token chunk][E][d] that
 // route_backward_sum_kernel adds in chunk order (one chunk: straight to the result).
-// Bound by memory (k + 2 rows per token); what costs is latency, so a tile asks for all of its rows before its first product, and
-// the first one's are under way while dz comes.  Forming dz here, once per column block, took 10 us more (8192 tokens of 2048 columns, 16
-// experts) than the launch of its own.
+// Bound by memory (k + 2 rows per token); what costs is latency, so a tile's rows are asked for ahead of the products of the tile before
+// it, the first one's while dz comes (8192 tokens of 2048 columns, 16 experts, two slots: 35 us, 3.9 TB/s; asked for behind those
+// products, with room for three workgroups per compute unit, 41).  Forming dz here, once per column block, took 10 us more than the launch of its own.
 // KK > 0: KK slots per token, their rows of a tile in flight together; KK == 0: any number, row by row.
 template <typename T, int NB, int KK>
-__global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(RouteBackward a, int chunk, int columns, int chunks)
+__global__ __launch_bounds__(256, NB == 1 ? 2 : 1) void route_backward_kernel(RouteBackward a, int chunk, int columns, int chunks)
 {
     constexpr int V = Store<T>::kVec, EP = 16 * NB, KN = KK > 0 ? KK : 1;
     extern __shared__ float lds[];                   // dz[chunk][EP] and 256 more, later the four wavefronts' sums of one block of experts
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(Ro
             const int tok = tok0 + t0 + 4 * g + v;
 #pragma unroll
             for (int j = 0; j < KN; ++j)
-                row[v][j] = KK > 0 && col_on && tok < a.T && dxp != nullptr ? a.inv[static_cast<size_t>(tok) * KN + j] : -1;
+                row[v][j] = KK > 0 && col_on && t0 < chunk && tok < a.T && dxp != nullptr ? a.inv[static_cast<size_t>(tok) * KN + j] : -1;
         }
     };
     auto ask_rows = [&](int t0) {
@@ -194,17 +194,36 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(Ro
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < V; ++j) accW[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    u32x4_t router[4 * NB];                          // experts past E: zeros, and dz too
+    auto ask_router = [&]() {
+#pragma unroll
+        for (int s = 0; s < 4 * NB; ++s) router[s] = router_row(4 * s + g);
+    };
+    if (NB == 1) ask_router();
+    ask_places(wave * 16 + 64);
     for (int t0 = wave * 16; t0 < chunk && tok0 + t0 < a.T; t0 += 64) {
         const int tok = tok0 + t0 + 4 * g;           // the lane's first token
+        if (NB > 1) ask_router();
+        u32x4_t xc[4], rc[4][KN];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            xc[v] = xv[v];
+#pragma unroll
+            for (int j = 0; j < KN; ++j) rc[v][j] = rv[v][j];
+        }
+        if (t0 + 64 < chunk) {
+            ask_rows(t0 + 64);
+            ask_places(t0 + 128);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         f32x4_t accX[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) accX[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 4 * NB; ++s) {           // (experts past E: dz and the router's row are zero)
-            const u32x4_t row = router_row(4 * s + g);
+        for (int s = 0; s < 4 * NB; ++s) {
             const float dz = lds[(t0 + m) * EP + 4 * s + g];
             float w[V];
-            Store<T>::unpack(row, w);
+            Store<T>::unpack(router[s], w);
 #pragma unroll
             for (int j = 0; j < V; ++j) accX[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(dz, w[j], accX[j], 0, 0, 0);
         }
@@ -212,7 +231,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(Ro
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 float f[V];
-                Store<T>::unpack(xv[v], f);
+                Store<T>::unpack(xc[v], f);
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     const float dz = lds[(t0 + 4 * g + v) * EP + m + 16 * b];
@@ -235,7 +254,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(Ro
             };
             if (KK > 0) {
 #pragma unroll
-                for (int j = 0; j < KN; ++j) add(rv[v][j]);
+                for (int j = 0; j < KN; ++j) add(rc[v][j]);
             } else if (dxp != nullptr) {
                 for (int j = 0; j < a.slots; ++j) {
                     const int row = a.inv[static_cast<size_t>(tok + v) * a.slots + j];
@@ -246,10 +265,6 @@ __global__ __launch_bounds__(256, NB == 1 ? 3 : 1) void route_backward_kernel(Ro
             for (int j = 0; j < V; ++j) sum[j] += accX[j][v];
             const uint4 packed = Store<T>::pack(sum);
             *reinterpret_cast<u32x4_t*>(dx + static_cast<size_t>(tok + v) * d + c) = u32x4_t{packed.x, packed.y, packed.z, packed.w};
-        }
-        if (t0 + 64 < chunk) {
-            ask_places(t0 + 64);
-            ask_rows(t0 + 64);
         }
     }
     if (a.dWg == nullptr) return;
