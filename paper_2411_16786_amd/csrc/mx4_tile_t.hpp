@@ -9,6 +9,8 @@
 // slice's come with two broadcast reads.
 // A workgroup of WN wavefronts owns BK = 64 WN columns of BR = 32 RT rows, a wavefront 64 columns: of its two blocks, block i has the
 // columns 2 c + i.  Stages of 64 n, two in the LDS, barrier ahead of the last slice as there.
+// Bound by the conversions and permutations beside the matrix instructions.  8192 rows over 8 experts, 64 x 256 tiles: 4608 -> 1152 106 to
+// 118 us, 1152 -> 4608 with the slope 122 to 134 (0.74 to 0.82 and 0.65 to 0.71 PFLOP/s).
 #pragma once
 #include "mx4_tile.hpp"
 

@@ -5,7 +5,7 @@
 // 1, 1.5, 2, 3, 4, 6 to |w| / s, ties to the even code (the conversion instruction's rounding).  w / s is exact: s is a power of two.
 //
 // Bound by memory: 32 columns are four lanes' 16-byte loads (bf16), the maximum goes round two lane exchanges, every lane
-// stores its eight codes as one dword.
+// stores its eight codes as one dword: 42 million bf16 weights with their values 34 us, 5.6 TB/s (partly from the memory-side cache; a copy 5.1).
 #include "kernels.hpp"
 #include "mx4.hpp"
 
