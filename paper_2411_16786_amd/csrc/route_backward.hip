@@ -327,12 +327,18 @@ __global__ __launch_bounds__(256) void route_backward_sum_kernel(const float* __
 
 namespace {
 
-// Tokens per workgroup: 64, one tile per wavefront, while that leaves two workgroups or less per compute unit; then up to 256 (128 with more
-// than 32 experts, whose dz has to fit the LDS), which keeps the partial sums a small part of what is read.
+// Tokens per workgroup: 64, one tile per wavefront, and up to 256 (128 with more than 32 experts, whose dz has to fit the LDS) while that
+// leaves two workgroups per compute unit, which keeps the partial sums a small part of what is read; with more than 32 chunks, whose
+// sum takes long, also while it leaves one (8 experts, 4096 tokens of 1152 columns, 64 and 32 chunks: 16.1 + 7.5 and 16.0 + 4.2 us; 16
+// experts, 8192 of 1792, 64 and 32: 34.9 + 7.8 and 32.4 + 4.8; 4096 of 2048, 32 and 16: 19.2 + 4.2 and 20.5 + 4.0).
 int route_chunk(int T_tok, int E, int columns)
 {
     int chunk = 64;
-    while (chunk < (E > 32 ? 128 : 256) && static_cast<long long>((T_tok + 2 * chunk - 1) / (2 * chunk)) * columns >= 2 * kComputeUnits) chunk *= 2;
+    while (chunk < (E > 32 ? 128 : 256)) {
+        const int least = (T_tok + chunk - 1) / chunk > 32 ? kComputeUnits : 2 * kComputeUnits;
+        if (static_cast<long long>((T_tok + 2 * chunk - 1) / (2 * chunk)) * columns < least) break;
+        chunk *= 2;
+    }
     return chunk;
 }
 

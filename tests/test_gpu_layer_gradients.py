@@ -30,6 +30,9 @@ SHAPES = [
     (3001, 64, 60, 2, 0, "bf16", 0.0),
     (2500, 32, 40, 1, 0, "f32", 0.1),
     (9000, 64, 4, 2, 0, "bf16", 0.0),
+    (4200, 2048, 16, 2, 0, "bf16", 0.1),                             # several tiles of tokens per wavefront
+    (4133, 2048, 40, 1, 0, "bf16", 0.0),
+    (2100, 1024, 8, 6, 1, "f32", 0.1),
     (513, 1152, 8, 2, 0, "bf16", 0.0),
 ]
 IDS = ["-".join(map(str, s)) for s in SHAPES]
