@@ -40,7 +40,7 @@ inline long long tile_count(int max_rows, int n_seg, int BM, int BN, int columns
 inline float tile_cost(long long tiles, int BM, int BN) { return static_cast<float>((tiles + kComputeUnits - 1) / kComputeUnits) * (BM * BN); }
 
 // Columns per wavefront set of mx4_rows_kernel: 16 while that gives each compute unit no more than six workgroups (4608 -> 1152, one token
-// 6.6 us against 9.6 with 32, eight tokens 9.1 and 10.0), else 32 (1152 -> 4608, eight tokens 9.2 against 11.6)
+// 6.0 us against 9.6 with 32, eight tokens 9.1 and 10.0), else 32 (1152 -> 4608, eight tokens 9.2 against 11.6)
 inline bool rows_narrow(int max_rows, int n_seg, int N) { return tile_bound(max_rows, n_seg, 16) * (N / 16) <= 6 * kComputeUnits; }
 
 // Float rows, which have no tiles: 64 columns and four shares instead of eight where that leaves each compute unit more than four
@@ -54,6 +54,8 @@ inline bool rows_wide(int max_rows, int n_seg, int N) { return tile_bound(max_ro
 // rates of 8192 -> 4096 of 8192 rows (444, 481 and 563 us; the tiles of 32 rows are for few rows); a compute unit with a single workgroup
 // of four wavefronts waits more.  Of the two of 32 rows, in shares, the narrower one in more shares while each tile has a compute unit
 // to itself (200 rows over 8 experts: 4608 -> 1152 13.4 us against 21.8, 1152 -> 4608, 288 tiles, 16.6 against 12.6).
+// Tiles of 64 rows in two shares while there are no more than 5/4 per compute unit (4608 -> 1152 over 8 experts, 1000 rows 29 us against
+// 35.5, 2000 rows, 315 tiles, 39 both; 300 rows over 16 experts, 8192 -> 2048, 53 against 62.5).
 inline int pick_tile(int max_rows, int n_seg, int N, int K)
 {
     if (max_rows <= 4 * n_seg && tile_bound(max_rows, n_seg, 16) * (N / 32) <= 12 * kComputeUnits) return -1;
@@ -75,8 +77,8 @@ inline int pick_tile(int max_rows, int n_seg, int N, int K)
 }
 
 // The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns of K; its LDS does not depend on the reduction).  4608 -> 1152, 8192
-// rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23.  1152 -> 4608,
-// 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
+// rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23, 1000 rows (315
+// tiles, 320 being 5/4 per compute unit) two shares 36, four 30.  1152 -> 4608, 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
 inline int pick_tile_t(int max_rows, int n_seg, int K)
 {
     if (max_rows <= 4 * n_seg && tile_bound(max_rows, n_seg, 16) * (K / 128) <= 12 * kComputeUnits) return -1;
