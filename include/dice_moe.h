@@ -345,11 +345,12 @@ int moe_ep_segments(moe_ctx* ctx, const int32_t* recv_counts, int32_t W, int32_t
  *
  * Format (OCP MXFP4): weight row n of a [rows][cols] array holds cols / 2 bytes of codes, column 2c in the low and column 2c + 1 in
  * the high half of byte c, and cols / 32 scale bytes, one per 32 columns.  Codes 0..7 stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 is the sign;
- * scale byte b stands for 2^(b - 127), 255 for NaN.  Expert arrays are W1_codes[E][F][d/2], W1_scales[E][F][d/32],
+ * scale byte b stands for 2^(b - 127), 255 for NaN; what would be 2^128 or more (b = 253 and 254) is infinite.  Expert arrays are W1_codes[E][F][d/2], W1_scales[E][F][d/32],
  * W2_codes[E][d][F/2], W2_scales[E][d][F/32] (E + n_shared experts with shared ones). */
 
 /* W[rows][cols] (dtype) to codes and scales: the scale of a group is the smallest power of two s >= 2^-126 with max|w| <= 7 s (larger
  * magnitudes than 6 s round to 6 s, no further off than the spacing there allows), a code is the nearest to w / s, ties to the even code.
+ * The largest scale is 2^125, so that codes of finite weights stand for numbers; magnitudes above 7 * 2^125 become 6 * 2^125.
  * A group that holds infinity or NaN gets scale byte 255 and codes 0.  values (dtype, may be NULL) receives what the codes stand for,
  * for training that sees the quantisation or for its error.
  *   rows >= 0, cols a multiple of 32, rows * cols <= 2^38; all of an expert array at once: rows = E * F */
@@ -357,7 +358,7 @@ int moe_quantize_mx4(moe_ctx* ctx, const void* W, int64_t rows, int32_t cols, ui
                      void* stream);
 
 /* moe_expert_ffn on 4-bit weights: u = W1_e . x + b1_e, h = W2_e . gelu(u) + b2_e for every row of every segment.  The weights
- * are exact in the products (a code with its scale is a bf16 value); sums are float, and gelu(u) is rounded to dtype once.
+ * are exact in the products (a code with its scale is a bf16 value, or infinite from 2^128 on); sums are float, and gelu(u) is rounded to dtype once.
  *   in : x_rows: packed rows (row_pairs NULL) or x[T][d] read through row_pairs as in moe_expert_ffn_rows;
  *        out_pairs: NULL, or the row of h_rows that packed row r goes to (distinct), as in moe_expert_ffn_commit: with
  *        moe_dispatch's perm and h_rows = H_cache, moe_combine with h_packed = NULL follows;

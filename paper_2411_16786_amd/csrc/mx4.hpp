@@ -1,7 +1,8 @@
 // 4-bit weights (OCP MXFP4): element codes E2M1, two per byte with the even column in the low half, and one power-of-two scale
 // byte (E8M0, 2^(byte - 127), 255 = NaN) per 32 columns of a row.  One instruction of gfx950 turns a byte of codes and a scale
 // into two values; a code has two significant bits and the scale is a power of two, so the values are exact in bf16 as in
-// float, and products on the matrix cores see the weights as they are.
+// float, and products on the matrix cores see the weights as they are.  (From 2^128 on they are infinite: codes of 4 and 6 under scale byte
+// 253, of 2 and more under 254, which the quantisation here never writes.)
 #pragma once
 #include "common.hpp"
 

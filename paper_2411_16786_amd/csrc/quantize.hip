@@ -1,8 +1,9 @@
 // Weights to 4-bit codes with one power-of-two scale per 32 columns (see mx4.hpp), and the values that the codes stand for.
 //
 // Scale: the smallest power of two s >= 2^-126 with max|w| <= 7 s.  A magnitude up to 7 s rounds to the largest code, 6 s, with at
-// most the error that the spacing there (4, 6) allows anyway, half of 2 s; any smaller s would clip.  Code: the nearest of 0, 0.5,
-// 1, 1.5, 2, 3, 4, 6 to |w| / s, ties to the even code (the conversion instruction's rounding).  w / s is exact: s is a power of two.
+// most the error that the spacing there (4, 6) allows anyway, half of 2 s; any smaller s would clip.  No s is above 2^125, where 6 s = 1.5 2^127
+// is the largest number that a code and a scale stand for: with 2^126 the code of 4 is infinite.  Code: the nearest of 0, 0.5,
+// 1, 1.5, 2, 3, 4, 6 to |w| / s, ties to the even code (the conversion instruction's rounding, which ends at 6).  w / s is exact: s is a power of two.
 //
 // Bound by memory: 32 columns are four lanes' 16-byte loads (bf16), the maximum goes round two lane exchanges, every lane
 // stores its eight codes as one dword: 42 million bf16 weights with their values 34 us, 5.6 TB/s (partly from the memory-side cache; a copy 5.1).
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(256) void quantize_mx4_kernel(const T* __restrict__
     // top = 1.f 2^(e - 127) is at most 7 s = 1.75 * 4 s for s = 2^(e - 127 - 2) where 1.f <= 1.75, for twice that otherwise
     const int e = static_cast<int>(top >> 23);
     int byte = e - ((top & 0x7FFFFFu) <= 0x600000u ? 2 : 1);
-    byte = byte < 1 ? 1 : byte;
+    byte = byte < 1 ? 1 : byte > 252 ? 252 : byte;
     const bool finite = e < 255;
     if (!finite) byte = 255;
     uint32_t c = 0;
