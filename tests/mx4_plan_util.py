@@ -51,3 +51,9 @@ def plan_t(rows, n_seg, K):
 def plans(rows, n_seg, d, F):
     """Of the forward's two products and of the gradient's two."""
     return plan(rows, n_seg, F, d), plan(rows, n_seg, d, F), plan_t(rows, n_seg, F), plan_t(rows, n_seg, d)
+
+
+def columns_left(kernel, N):
+    """Columns of N behind the last whole block of a kernel, by its name."""
+    block = {"rows16": 16, "rows32": 32, "rows64": 64, "rows": 128}.get(kernel)
+    return N % (block or int(kernel.rstrip("+").split("/")[0].split("x")[1]))

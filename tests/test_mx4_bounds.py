@@ -6,9 +6,10 @@ import torch
 import mx4_stage_util as S
 import mx4_util as M
 import test_gpu_mx4
+import test_gpu_mx4_partial_columns
 import test_gpu_mx4_tiles
 
-WIDTHS = sorted({("bf16", s[1], s[2]) for s in test_gpu_mx4_tiles.SHAPES} | {(c[5], c[1], c[2]) for c in test_gpu_mx4.CASES})
+WIDTHS = sorted({("bf16", s[1], s[2]) for s in test_gpu_mx4_tiles.SHAPES + test_gpu_mx4_partial_columns.PARTIAL} | {(c[5], c[1], c[2]) for c in test_gpu_mx4.CASES})
 ROWS = 8
 
 
