@@ -270,8 +270,8 @@ int moe_expert_ffn_status(moe_ctx* ctx, const void* workspace, void* stream);
 
 /* Measurement aids (they compute nothing of the method; the benchmark uses them to print the
  * per-GEMM split of the expert FFN and the machine ceilings its roofline fractions are read against).
- * moe_expert_ffn_between_event: from now on every expert FFN call of this context records `event` (a
- *   hipEvent_t owned by the caller, or NULL to stop) on its stream between its two grouped GEMMs.
+ * moe_expert_ffn_between_event: from now on every expert FFN call of this context (moe_expert_ffn_mx4 and its gradient
+ *   included) records `event` (a hipEvent_t owned by the caller, or NULL to stop) on its stream between its two grouped GEMMs.
  * moe_calibrate_copy: a plain streaming copy of `bytes` (multiple of 16) device bytes with `workgroups`
  *   workgroups of 256 lanes, 16 bytes per lane.
  * moe_calibrate_mfma: a register-resident loop of `iters` x 8 bf16 MFMAs (32x32x16) per wavefront, four

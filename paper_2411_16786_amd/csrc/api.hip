@@ -589,7 +589,8 @@ int moe_expert_ffn_mx4(moe_ctx* ctx, const void* x_rows, const int32_t* row_pair
     int32_t* const status = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + status_offset(ctx));
     return hip_result(ctx,
                       launch_expert_ffn_mx4(is_bf16(ctx), x_rows, row_pairs, slots(ctx), seg, s.d, s.F, {W1_codes, W1_scales}, b1,
-                                            {W2_codes, W2_scales}, b2, u_packed, h_rows, out_pairs, workspace, status, static_cast<hipStream_t>(stream)),
+                                            {W2_codes, W2_scales}, b2, u_packed, h_rows, out_pairs, workspace, status, static_cast<hipStream_t>(stream),
+                                            ctx->ffn_between),
                       who);
 }
 
@@ -611,7 +612,7 @@ int moe_expert_ffn_mx4_backward(moe_ctx* ctx, const void* dh_packed, const void*
     return hip_result(ctx,
                       launch_expert_ffn_mx4_backward(is_bf16(ctx), dh_packed, u_packed, seg, s.d, s.F, {W1_codes, W1_scales},
                                                      {W2_codes, W2_scales}, du_packed ? du_packed : workspace, dx_packed, status,
-                                                     static_cast<hipStream_t>(stream)),
+                                                     static_cast<hipStream_t>(stream), ctx->ffn_between),
                       who);
 }
 

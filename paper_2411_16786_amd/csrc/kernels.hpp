@@ -101,15 +101,15 @@ hipError_t launch_quantize_mx4(bool bf16, const void* W, long long rows, int col
 struct Mx4 { const uint8_t* codes; const uint8_t* scales; };
 // The rows of a grouped product and where they belong.  Rows at and beyond max_rows are not touched.
 struct Segments { const int32_t* offsets; const int32_t* expert; int n, n_experts, max_rows; };
-// launch_expert_ffn on 4-bit weights; pre (may be null) receives the pre-activations [rows][F]
+// launch_expert_ffn on 4-bit weights; pre (may be null) receives the pre-activations [rows][F]; between as there
 hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
                                  const Mx4& W1, const float* b1, const Mx4& W2, const float* b2, void* pre, void* h_out,
-                                 const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream);
+                                 const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream, hipEvent_t between);
 // Once per device before the first of these launches there: raises the dynamic-LDS limit of the tiled kernels.
 hipError_t prepare_expert_ffn_mx4();
 // du = (dh W2) gelu'(u), dx = du W1, row by row of the packed order
 hipError_t launch_expert_ffn_mx4_backward(bool bf16, const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1,
-                                          const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream);
+                                          const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream, hipEvent_t between);
 
 hipError_t launch_combine_backward(bool bf16, const void* dy, const void* h_packed, const int32_t* inv, const float* scores, int T_tok,
                                    int d, int k, void* dh_packed, float* dscores, hipStream_t stream);

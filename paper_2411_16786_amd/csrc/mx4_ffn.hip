@@ -349,20 +349,25 @@ void transposed_product(const void* y, const Segments& seg, int N, int K, const 
 
 template <typename T>
 hipError_t ffn_t(const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F, const Mx4& W1, const float* b1,
-                 const Mx4& W2, const float* b2, void* pre, void* h_out, const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream)
+                 const Mx4& W2, const float* b2, void* pre, void* h_out, const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream,
+                 hipEvent_t between)
 {
     rows_product<T, true>(x_rows, row_index, row_div, seg, F, d, W1, b1, pre, hidden, nullptr, status, stream);
     if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+    if (between != nullptr)
+        if (hipError_t err = hipEventRecord(between, stream); err != hipSuccess) return err;
     rows_product<T, false>(hidden, nullptr, 1, seg, d, F, W2, b2, nullptr, h_out, out_index, nullptr, stream);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t ffn_backward_t(const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1, const Mx4& W2, void* du, void* dx,
-                          int32_t* status, hipStream_t stream)
+                          int32_t* status, hipStream_t stream, hipEvent_t between)
 {
     transposed_product<T, true>(dh, seg, d, F, W2, u, du, status, stream);
     if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+    if (between != nullptr)
+        if (hipError_t err = hipEventRecord(between, stream); err != hipSuccess) return err;
     transposed_product<T, false>(du, seg, F, d, W1, nullptr, dx, nullptr, stream);
     return hipGetLastError();
 }
@@ -386,15 +391,15 @@ hipError_t prepare_expert_ffn_mx4()
 
 hipError_t launch_expert_ffn_mx4(bool bf16, const void* x_rows, const int32_t* row_index, int row_div, const Segments& seg, int d, int F,
                                  const Mx4& W1, const float* b1, const Mx4& W2, const float* b2, void* pre, void* h_out,
-                                 const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream)
+                                 const int32_t* out_index, void* hidden, int32_t* status, hipStream_t stream, hipEvent_t between)
 {
-    return (bf16 ? ffn_t<bf16_t> : ffn_t<float>)(x_rows, row_index, row_div, seg, d, F, W1, b1, W2, b2, pre, h_out, out_index, hidden, status, stream);
+    return (bf16 ? ffn_t<bf16_t> : ffn_t<float>)(x_rows, row_index, row_div, seg, d, F, W1, b1, W2, b2, pre, h_out, out_index, hidden, status, stream, between);
 }
 
 hipError_t launch_expert_ffn_mx4_backward(bool bf16, const void* dh, const void* u, const Segments& seg, int d, int F, const Mx4& W1,
-                                          const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream)
+                                          const Mx4& W2, void* du, void* dx, int32_t* status, hipStream_t stream, hipEvent_t between)
 {
-    return (bf16 ? ffn_backward_t<bf16_t> : ffn_backward_t<float>)(dh, u, seg, d, F, W1, W2, du, dx, status, stream);
+    return (bf16 ? ffn_backward_t<bf16_t> : ffn_backward_t<float>)(dh, u, seg, d, F, W1, W2, du, dx, status, stream, between);
 }
 
 }  // namespace dicemoe
