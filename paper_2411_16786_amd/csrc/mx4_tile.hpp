@@ -34,7 +34,7 @@ __device__ __forceinline__ float normal_tail(float a) {
 }
 // gelu and its slope.  The bf16 forms use that polynomial; NaN stays NaN in all of them.
 template <typename T> __device__ __forceinline__ float mx4_gelu(float u);
-template <> __device__ __forceinline__ float mx4_gelu<float>(float u) { return gelu_erf(u); }
+template <> __device__ __forceinline__ float mx4_gelu<float>(float u) { return u < -40.0f ? 0.0f : gelu_erf(u); }     // (-infinity times its zero is no number)
 template <> __device__ __forceinline__ float mx4_gelu<bf16_t>(float u) { return u != u ? u : gelu_erf_fast(u); }
 // gelu'(u) = Phi(u) + u phi(u); with a = |u| it is 1 - s for u >= 0 and s below, s = Phi(-a) - a phi(a)
 template <typename T> __device__ __forceinline__ float gelu_slope(float u);

@@ -1,13 +1,15 @@
-"""4-bit experts at the ends of the number range: the largest weights."""
-
+"""4-bit experts at the ends of the number range: the largest weights, infinite pre-activations."""
 import numpy as np
 import pytest
 import torch
 
+import mx4_stage_util as S
 import mx4_util as M
 from paper_2411_16786_amd import binding as B
 
 pytestmark = pytest.mark.gpu
+
+INF = float("inf")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -34,3 +36,60 @@ def test_the_largest_weights_stand_for_numbers(dtype):
     code = even[np.argmin(np.abs(v[..., None] - M.MAGNITUDE[even]), axis=-1)]
     assert np.array_equal(np.abs(got), M.MAGNITUDE[code] * step)
     assert np.array_equal(np.signbit(got), np.signbit(w.numpy()))
+
+
+class Ends:
+    """Rows through designed weights of one expert, d = 64, F = 128, all scales 1."""
+
+    def __init__(self, T, dtype):
+        self.T, self.dtype, self.dt = T, dtype, M.DT[dtype]
+        self.ctx = B.Context(T, 64, 128, 1, 1, dtype)
+        self.seg, self.one = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([0, T], [0]))
+        self.ws = torch.empty(self.ctx.workspace_bytes(), dtype=torch.uint8, device="cuda")
+
+    @staticmethod
+    def weights(code):
+        """codes [rows, cols] 0 .. 15 as the calls take them."""
+        code = code.to(torch.uint8)
+        return (code[:, 0::2] | (code[:, 1::2] << 4)).contiguous()[None].cuda(), torch.full((1, code.shape[0], code.shape[1] // 32), 127, dtype=torch.uint8).cuda()
+
+    def forward(self, x, W1, W2):
+        u, h = (torch.full((self.T, n), 3.0, dtype=self.dt, device="cuda") for n in (128, 64))
+        self.ctx.moe_expert_ffn_mx4(x.to(self.dt).cuda(), None, None, self.seg, self.one, self.T, W1, None, W2, None, u, h, self.ws)
+        kept = S.stored_hidden(self.ws, self.T, 128, self.dt).cpu().double()
+        return u.cpu().double(), kept, h.cpu().double()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [4, 300])
+def test_infinite_pre_activations(dtype, T):
+    """Sums that overflow are infinite, gelu of -infinity is (near) zero, and the second product gives what arithmetic with infinities gives."""
+    c = Ends(T, dtype)
+    gen = torch.Generator().manual_seed(T)
+    n = torch.arange(128)
+    code1 = torch.randint(0, 8, (128, 64), generator=gen)           # column 0: 0, 4, -4, 2 in turn; column 1: -4
+    code1[:, 0], code1[:, 1] = torch.tensor([0, 6, 14, 4])[n % 4], 14
+    x = torch.zeros((T, 64))
+    kind = torch.arange(T) % 4
+    x[kind == 0, 0], x[kind == 1, 0], x[kind == 2, 1], x[kind == 3, 0] = 3e38, -3e38, 3e38, 0.5
+    code2 = torch.randint(0, 16, (64, 128), generator=gen)
+    code2[0], code2[1], code2[2] = 4, 12, 0                         # 2, -2 and 0 everywhere
+    code2[3] = torch.tensor([4, 4, 4, 12])[n % 4]                   # 2, 2, 2, -2
+    code2[4] = torch.where(n % 4 == 2, 0, 4)
+    u, kept, h = c.forward(x, c.weights(code1), c.weights(code2))
+    ends = torch.tensor([0.0, INF, -INF, INF])[n % 4].double()
+    assert torch.isinf(u).any()
+    assert torch.equal(u[kind == 0], ends.expand(int((kind == 0).sum()), 128)) and torch.equal(u[kind == 1], -ends.expand(int((kind == 1).sum()), 128))
+    assert (u[kind == 2] == -INF).all()
+    assert not torch.isnan(kept).any()
+    assert torch.equal(torch.isinf(kept), u == INF) and (kept[u == -INF].abs() < 1e-8).all()
+    up = h[kind == 0]                                               # infinite where n % 4 is 1 or 3
+    assert (up[:, 0] == INF).all() and (up[:, 1] == -INF).all() and torch.isnan(up[:, 2:4]).all() and (up[:, 4] == INF).all()
+    down = h[kind == 1]                                             # ... where it is 2
+    assert (down[:, 0] == INF).all() and (down[:, 1] == -INF).all() and torch.isnan(down[:, 2]).all() and (down[:, 3] == INF).all() and torch.isnan(down[:, 4]).all()
+    assert (h[kind == 2].abs() < 1e-5).all()                        # 128 terms of 6e-9 times 6 at most
+    small = h[kind == 3]
+    g, v2 = M.gelu(torch.tensor([0.0, 2.0, -2.0, 1.0]).double())[n % 4], torch.from_numpy(M.CODE_VALUE[code2.numpy()])
+    want, size = v2 @ g, v2.abs() @ g.abs()
+    off = (M.HALF[dtype] + 130 * 2.0 ** -23) * size + 1e-6 * v2.abs().sum(1)        # one rounding of the hidden value, the sum, the form of GELU
+    assert ((small - want).abs() <= off + M.HALF[dtype] * (want.abs() + off)).all()
