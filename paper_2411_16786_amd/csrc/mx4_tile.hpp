@@ -32,15 +32,19 @@ __device__ __forceinline__ float normal_tail(float a) {
     p = fmaf(p, a, -0x1.ffff18p-1f);
     return __builtin_amdgcn_exp2f(p);
 }
-// gelu and its slope.  The bf16 forms use that polynomial; NaN stays NaN in all of them.
+// gelu and its slope.  The float forms take Phi(u) from erfc, which keeps its digits where Phi is small (1 + erf, a difference there, is off
+// by 4 % of itself at u = -5 and by half at -5.5); the bf16 forms use that polynomial; NaN stays NaN in all of them.
 template <typename T> __device__ __forceinline__ float mx4_gelu(float u);
-template <> __device__ __forceinline__ float mx4_gelu<float>(float u) { return u < -40.0f ? 0.0f : gelu_erf(u); }     // (-infinity times its zero is no number)
+template <> __device__ __forceinline__ float mx4_gelu<float>(float u) {
+    const float c = u < -40.0f ? -40.0f : u;                    // (-infinity times its zero is no number; gelu is zero from -15 on)
+    return 0.5f * c * erfcf(c * -0.70710678118654752440f);
+}
 template <> __device__ __forceinline__ float mx4_gelu<bf16_t>(float u) { return u != u ? u : gelu_erf_fast(u); }
 // gelu'(u) = Phi(u) + u phi(u); with a = |u| it is 1 - s for u >= 0 and s below, s = Phi(-a) - a phi(a)
 template <typename T> __device__ __forceinline__ float gelu_slope(float u);
 template <> __device__ __forceinline__ float gelu_slope<float>(float u) {
     const float a = fminf(fabsf(u), 40.0f);                     // (infinity times the bell's zero is no number; u phi(u) is zero from 15 on)
-    return 0.5f * (1.0f + erff(u * 0.70710678118654752440f)) + copysignf(a, u) * (0.39894228040143267794f * expf(-0.5f * a * a));
+    return 0.5f * erfcf(u * -0.70710678118654752440f) + copysignf(a, u) * (0.39894228040143267794f * expf(-0.5f * a * a));
 }
 template <> __device__ __forceinline__ float gelu_slope<bf16_t>(float u) {
     const float a = fminf(fabsf(u), 6.0f);

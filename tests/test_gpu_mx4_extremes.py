@@ -1,4 +1,6 @@
-"""4-bit experts at the ends of the number range: the largest weights, infinite pre-activations."""
+"""4-bit experts at the ends of the number range: the largest weights, infinite pre-activations, the tails of the float GELU and its slope."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -59,6 +61,17 @@ class Ends:
         kept = S.stored_hidden(self.ws, self.T, 128, self.dt).cpu().double()
         return u.cpu().double(), kept, h.cpu().double()
 
+    def slopes(self, u):
+        """gelu'(u) [T, 128] through a gradient whose product is exactly 1 everywhere."""
+        code = torch.zeros((64, 128))
+        code[0] = 2                                                 # the first row of W2 holds ones, and dh selects it
+        dh = torch.zeros((self.T, 64))
+        dh[:, 0] = 1.0
+        du, dx = (torch.empty((self.T, n), dtype=self.dt, device="cuda") for n in (128, 64))
+        self.ctx.moe_expert_ffn_mx4_backward(dh.to(self.dt).cuda(), u.to(self.dt).cuda(), self.seg, self.one, self.T, self.weights(torch.zeros((128, 64))),
+                                             self.weights(code), du, dx, self.ws)
+        return du.cpu().double()
+
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T", [4, 300])
@@ -93,3 +106,36 @@ def test_infinite_pre_activations(dtype, T):
     want, size = v2 @ g, v2.abs() @ g.abs()
     off = (M.HALF[dtype] + 130 * 2.0 ** -23) * size + 1e-6 * v2.abs().sum(1)        # one rounding of the hidden value, the sum, the form of GELU
     assert ((small - want).abs() <= off + M.HALF[dtype] * (want.abs() + off)).all()
+
+
+@pytest.mark.parametrize("T", [7, 300])
+def test_float_gelu_keeps_its_digits_in_the_tail(T):
+    """Relative to gelu(u) = u Phi(u), u from -12 to 0: erfc(x), x = -u / sqrt 2, amplifies the two roundings of x by at most 2 x^2 + 1 = u^2 + 1
+    each; 16 half steps for erfc itself and the products."""
+    c = Ends(T, "f32")
+    u = -12.0 * torch.rand(T, generator=torch.Generator().manual_seed(T))
+    u[0], u[1], u[2] = -5.0, -5.5, -12.0
+    code1 = torch.zeros((128, 64))
+    code1[:, 0] = 2
+    x = torch.zeros((T, 64))
+    x[:, 0] = u
+    got_u, kept, _ = c.forward(x, c.weights(code1), c.weights(torch.zeros((64, 128))))
+    v = u.double()[:, None].expand(T, 128)
+    assert torch.equal(got_u, v)
+    want = M.gelu(v)
+    assert ((kept - want).abs() <= (2 * (v * v + 1) + 16) * 2.0 ** -24 * want.abs()).all(), S.excess(kept, want, 2.0 ** -24 * want.abs())
+
+
+@pytest.mark.parametrize("T", [7, 300])
+def test_float_slope_keeps_its_digits_in_the_tail(T):
+    """Relative to Phi(u) + |u| phi(u), u from -12 to 12: as above for Phi; the exponent u^2 / 2 of phi has two roundings, so u^2 half steps,
+    and 16 more for exp and the products."""
+    c = Ends(T, "f32")
+    u = torch.linspace(-12.0, 12.0, T * 128).reshape(T, 128)
+    u[0, :4] = torch.tensor([-5.0, -5.5, -6.0, -0.75])
+    got, v = c.slopes(u), u.double()
+    phi = torch.exp(-0.5 * v * v) / math.sqrt(2.0 * math.pi)
+    Phi = 0.5 * torch.erfc(-v / math.sqrt(2.0))
+    tol = ((2 * (v * v + 1) + 16) * Phi + (v * v + 16) * v.abs() * phi) * 2.0 ** -24
+    want = Phi + v * phi
+    assert ((got - want).abs() <= tol).all(), S.excess(got, want, tol)
