@@ -49,7 +49,7 @@ template <> __device__ __forceinline__ float gelu_slope<float>(float u) {
 template <> __device__ __forceinline__ float gelu_slope<bf16_t>(float u) {
     const float a = fminf(fabsf(u), 6.0f);
     const float bell = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * a * a);
-    const float s = normal_tail(a) - a * bell;
+    const float s = a < 6.0f ? normal_tail(a) - a * bell : 0.0f;        // (-3.6e-8 at 6, and zero soon after)
     return u != u ? u : (u >= 0.0f ? 1.0f - s : s);
 }
 

@@ -1,4 +1,4 @@
-"""4-bit experts at the ends of the number range: the largest weights, infinite pre-activations, the tails of the float GELU and its slope."""
+"""4-bit experts at the ends of the number range: the largest weights, infinite pre-activations, the tails of GELU and of its slope."""
 import math
 
 import numpy as np
@@ -139,3 +139,11 @@ def test_float_slope_keeps_its_digits_in_the_tail(T):
     tol = ((2 * (v * v + 1) + 16) * Phi + (v * v + 16) * v.abs() * phi) * 2.0 ** -24
     want = Phi + v * phi
     assert ((got - want).abs() <= tol).all(), S.excess(got, want, tol)
+
+
+@pytest.mark.parametrize("T", [7, 300])
+def test_bf16_slope_beyond_its_polynomial(T):
+    """gelu' is below 1e-13 in magnitude from -8 on and as near to 1 from 8 on: 0 and 1 in bf16."""
+    c = Ends(T, "bf16")
+    u = torch.tensor([-8.0, -9.5, -60.0, -1e30, -INF, 8.0, 9.5, 60.0, 1e30, INF])[torch.arange(T * 128) % 10].reshape(T, 128)
+    assert torch.equal(c.slopes(u).abs(), (u > 0).double())
