@@ -36,15 +36,23 @@ __device__ __forceinline__ float gelu_erf(float u) {
 // result is within 3e-7 of the exact GELU everywhere, four orders of magnitude under the bf16 rounding
 // (2^-9 relative) that it receives next.  Cost: one transcendental (exp2) and nine plain operations; the
 // epilogue of the first GEMM evaluates it 4608 times per row.
-__device__ __forceinline__ float gelu_erf_fast(float u) {
-    const float a = fminf(fabsf(u), 6.0f);
+__device__ __forceinline__ float gelu_erf_fast(float u);
+
+// Phi(-a) of a = |u| up to 6, which it also leaves in a
+__device__ __forceinline__ float normal_tail(float u, float& a) {
+    a = fminf(fabsf(u), 6.0f);
     float p = fmaf(0x1.159ab2p-15f, a, -0x1.934b26p-11f);
     p = fmaf(p, a, 0x1.08ca02p-7f);
     p = fmaf(p, a, -0x1.b58d52p-5f);
     p = fmaf(p, a, -0x1.d5c80ep-2f);
     p = fmaf(p, a, -0x1.26b528p+0f);
     p = fmaf(p, a, -0x1.ffff18p-1f);
-    const float tail = __builtin_amdgcn_exp2f(p);            // Phi(-a)
+    return __builtin_amdgcn_exp2f(p);
+}
+
+__device__ __forceinline__ float gelu_erf_fast(float u) {
+    float a;
+    const float tail = normal_tail(u, a);
     return fmaf(-a, tail, fmaxf(u, 0.0f));
 }
 

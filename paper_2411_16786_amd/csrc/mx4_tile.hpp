@@ -22,18 +22,8 @@
 
 namespace dicemoe {
 
-// Phi(-a) for a in 0 .. 6: the polynomial that gelu_erf_fast has in its body
-__device__ __forceinline__ float normal_tail(float a) {
-    float p = fmaf(0x1.159ab2p-15f, a, -0x1.934b26p-11f);
-    p = fmaf(p, a, 0x1.08ca02p-7f);
-    p = fmaf(p, a, -0x1.b58d52p-5f);
-    p = fmaf(p, a, -0x1.d5c80ep-2f);
-    p = fmaf(p, a, -0x1.26b528p+0f);
-    p = fmaf(p, a, -0x1.ffff18p-1f);
-    return __builtin_amdgcn_exp2f(p);
-}
 // gelu and its slope.  The float forms take Phi(u) from erfc, which keeps its digits where Phi is small (1 + erf, a difference there, is off
-// by 4 % of itself at u = -5 and by half at -5.5); the bf16 forms use that polynomial; NaN stays NaN in all of them.
+// by 4 % of itself at u = -5 and by half at -5.5); the bf16 forms use normal_tail's polynomial; NaN stays NaN in all of them.
 template <typename T> __device__ __forceinline__ float mx4_gelu(float u);
 template <> __device__ __forceinline__ float mx4_gelu<float>(float u) {
     const float c = u < -40.0f ? -40.0f : u;                    // (-infinity times its zero is no number; gelu is zero from -15 on)
@@ -47,9 +37,10 @@ template <> __device__ __forceinline__ float gelu_slope<float>(float u) {
     return 0.5f * erfcf(u * -0.70710678118654752440f) + copysignf(a, u) * (0.39894228040143267794f * expf(-0.5f * a * a));
 }
 template <> __device__ __forceinline__ float gelu_slope<bf16_t>(float u) {
-    const float a = fminf(fabsf(u), 6.0f);
+    float a;
+    const float tail = normal_tail(u, a);
     const float bell = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * a * a);
-    const float s = a < 6.0f ? normal_tail(a) - a * bell : 0.0f;        // (-3.6e-8 at 6, and zero soon after)
+    const float s = a < 6.0f ? tail - a * bell : 0.0f;          // (-3.6e-8 at 6, and zero soon after)
     return u != u ? u : (u >= 0.0f ? 1.0f - s : s);
 }
 
