@@ -21,11 +21,12 @@ template <int RT, int WN, int KS> struct TileShapeT {
     static constexpr int kRowBytes = BR * 128, kCodePitch = BK / 2, kCodeBytes = 64 * kCodePitch;
     static constexpr int kScalePitch = 80, kScaleBytes = 2 * WN * kScalePitch * 4;        // (64 floats and 16 more: two groups and two halves on banks of their own)
     static constexpr int kRowLoads = kRowBytes / 16 / kThreads, kCodeLoads = kCodeBytes / 16 / kThreads;
+    static_assert(WN == 2 || WN == 4, "the swizzles below");
     static_assert(kRowBytes % (16 * kThreads) == 0 && kCodeBytes % (16 * kThreads) == 0, "whole loads");
     static constexpr int kShareBytes = 2 * (kRowBytes + kCodeBytes + kScaleBytes), kSumBytes = (KS - 1) * 2 * RT * 64 * kThreads;
     static constexpr int kLds = KS * kShareBytes > kSumBytes ? KS * kShareBytes : kSumBytes;
     // 16-byte chunk c of row n of the codes lies at place c ^ swizzle(n): transposing reads of 16 rows then spread over all banks
-    __device__ static constexpr int swizzle(int n) { return WN == 8 ? 2 * (n & 7) : WN == 4 ? (n >> 1) & 7 : (n >> 2) & 3; }
+    __device__ static constexpr int swizzle(int n) { return WN == 4 ? (n >> 1) & 7 : (n >> 2) & 3; }
 };
 
 template <int RT, int WN, int KS, bool SLOPE>
