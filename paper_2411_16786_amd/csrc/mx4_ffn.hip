@@ -241,8 +241,18 @@ __global__ __launch_bounds__(KS * kWave) void mx4_rows_transposed_kernel(const T
 
 namespace {
 
-// A tile as its kernel takes it: 32 RT rows, 32 WN columns (64 WN in the transposed kernel), the reduction in KS shares
+// A tile of the plan as its kernel takes it: 32 RT rows, 32 WN columns (64 WN in the transposed kernel), the reduction in KS shares
 template <int RT_, int WN_, int KS_> struct Tile { static constexpr int RT = RT_, WN = WN_, KS = KS_; };
+template <int I> using PlanTile = Tile<kTile[I].rows / 32, kTile[I].columns / 32, kTile[I].shares>;
+template <int I> using PlanTileT = Tile<kTileT[I].rows / 32, kTileT[I].columns / 64, kTileT[I].shares>;
+
+// the LDS that the plan weighs a tile by is what its kernel takes
+template <int I, int K> constexpr bool kLdsAsPlanned =
+    TileShape<PlanTile<I>::RT, PlanTile<I>::WN, PlanTile<I>::KS, false>::lds_bytes(K) == tile_lds(I, K, false) &&
+    TileShape<PlanTile<I>::RT, PlanTile<I>::WN, PlanTile<I>::KS, true>::lds_bytes(K) == tile_lds(I, K, true);
+template <int I> constexpr bool kTileAsPlanned = kTile[I].rows % 32 == 0 && kTile[I].columns % 32 == 0 && kLdsAsPlanned<I, 64> && kLdsAsPlanned<I, 1152> && kLdsAsPlanned<I, 8192>;
+static_assert(kTiles == 6 && kTileAsPlanned<0> && kTileAsPlanned<1> && kTileAsPlanned<2> && kTileAsPlanned<3> && kTileAsPlanned<4> && kTileAsPlanned<5>, "mx4_plan.hpp");
+static_assert(kTilesT == 3, "with_tile_t");
 
 // Calls f with the shape of a tile and whether its scales go by chunks
 template <typename F>
@@ -253,20 +263,20 @@ void with_tile(int tile, int K, F&& f)
         if (chunks) f(shape, std::true_type{});
         else f(shape, std::false_type{});
     };
-    if (tile == 0) go(Tile<4, 8, 1>{});
-    else if (tile == 1) go(Tile<4, 4, 1>{});
-    else if (tile == 2) go(Tile<2, 4, 1>{});
-    else if (tile == 3) go(Tile<1, 4, 2>{});
-    else if (tile == 4) go(Tile<1, 2, 4>{});
-    else go(Tile<2, 4, 2>{});
+    if (tile == 0) go(PlanTile<0>{});
+    else if (tile == 1) go(PlanTile<1>{});
+    else if (tile == 2) go(PlanTile<2>{});
+    else if (tile == 3) go(PlanTile<3>{});
+    else if (tile == 4) go(PlanTile<4>{});
+    else go(PlanTile<5>{});
 }
 
 template <typename F>
 void with_tile_t(int tile, F&& f)
 {
-    if (tile == 0) f(Tile<2, 4, 1>{});
-    else if (tile == 1) f(Tile<1, 2, 2>{});
-    else f(Tile<1, 2, 4>{});
+    if (tile == 0) f(PlanTileT<0>{});
+    else if (tile == 1) f(PlanTileT<1>{});
+    else f(PlanTileT<2>{});
 }
 
 template <typename Shape>
@@ -322,7 +332,7 @@ void transposed_product(const void* y, const Segments& seg, int N, int K, const 
             with_tile_t(tile, [&](auto shape) {
                 constexpr int RT = decltype(shape)::RT, WN = decltype(shape)::WN, KS = decltype(shape)::KS;
                 typedef TileShapeT<RT, WN, KS> S;
-                static_assert(KS == 4 || S::kLds <= 64 * 1024, "no raised limit");
+                static_assert(KS == PlanTileT<2>::KS || S::kLds <= 64 * 1024, "prepare_expert_ffn_mx4 raises the limit of that one");
                 const long long blocks = (tile_bound(seg.max_rows, seg.n, S::BR) * ((K + S::BK - 1) / S::BK) + 7) / 8 * 8;
                 hipLaunchKernelGGL((mx4_tile_transposed_kernel<RT, WN, KS, SLOPE>), dim3(static_cast<unsigned>(blocks)), dim3(KS * S::kThreads), S::kLds, stream,
                                    static_cast<const T*>(y), seg, N, K, W, static_cast<const T*>(u), static_cast<T*>(out), status);
@@ -376,14 +386,15 @@ hipError_t ffn_backward_t(const void* dh, const void* u, const Segments& seg, in
 
 hipError_t prepare_expert_ffn_mx4()
 {
-    hipError_t err = configure_tile<Tile<4, 8, 1>>();
-    if (err == hipSuccess) err = configure_tile<Tile<4, 4, 1>>();
-    if (err == hipSuccess) err = configure_tile<Tile<2, 4, 1>>();
-    if (err == hipSuccess) err = configure_tile<Tile<1, 4, 2>>();
-    if (err == hipSuccess) err = configure_tile<Tile<1, 2, 4>>();
-    if (err == hipSuccess) err = configure_tile<Tile<2, 4, 2>>();
-    const auto shares = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<1, 2, 4, false>);
-    const auto shares_slope = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<1, 2, 4, true>);
+    hipError_t err = configure_tile<PlanTile<0>>();
+    if (err == hipSuccess) err = configure_tile<PlanTile<1>>();
+    if (err == hipSuccess) err = configure_tile<PlanTile<2>>();
+    if (err == hipSuccess) err = configure_tile<PlanTile<3>>();
+    if (err == hipSuccess) err = configure_tile<PlanTile<4>>();
+    if (err == hipSuccess) err = configure_tile<PlanTile<5>>();
+    typedef PlanTileT<2> Shares;
+    const auto shares = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<Shares::RT, Shares::WN, Shares::KS, false>);
+    const auto shares_slope = reinterpret_cast<const void*>(&mx4_tile_transposed_kernel<Shares::RT, Shares::WN, Shares::KS, true>);
     for (const void* kernel : {shares, shares_slope})            // (the other transposed tiles need less than the 64 KiB that every kernel has)
         if (err == hipSuccess) err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
     return err;

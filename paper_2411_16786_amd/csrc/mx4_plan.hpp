@@ -22,7 +22,7 @@ constexpr TileSize kTile[kTiles] = {{128, 256, 1}, {128, 128, 1}, {64, 128, 1}, 
 
 // Scales by chunks where all of them at once would leave less than three workgroups per compute unit: 4608 -> 1152 with 256 x 128
 // tiles 103 us instead of 113 and with 128 x 128 92 instead of 103, but with 128 x 64, where they leave three, 104 instead of 93
-inline int tile_lds(int tile, int K, bool chunks)
+constexpr int tile_lds(int tile, int K, bool chunks)
 {
     const TileSize t = kTile[tile];
     const int unit = 32 * t.columns * t.shares;                  // a workgroup's 16-byte loads
@@ -79,11 +79,14 @@ inline int pick_tile(int max_rows, int n_seg, int N, int K)
 // The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns of K; its LDS does not depend on the reduction).  4608 -> 1152, 8192
 // rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23, 1000 rows (315
 // tiles, 320 being 5/4 per compute unit) two shares 36, four 30.  1152 -> 4608, 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
+constexpr int kTilesT = 3;
+constexpr TileSize kTileT[kTilesT] = {{64, 256, 1}, {32, 128, 2}, {32, 128, 4}};
 inline int pick_tile_t(int max_rows, int n_seg, int K)
 {
+    constexpr TileSize large_tile = kTileT[0], small_tile = kTileT[1];
     if (max_rows <= 4 * n_seg && tile_bound(max_rows, n_seg, 16) * (K / 128) <= 12 * kComputeUnits) return -1;
-    const long long large = tile_count(max_rows, n_seg, 64, 256, K), small = tile_count(max_rows, n_seg, 32, 128, K);
-    if (tile_cost(large, 64, 256) * (large <= kComputeUnits ? 1.3f : 1.0f) <= 1.6f * tile_cost(small, 32, 128)) return 0;
+    const long long large = tile_count(max_rows, n_seg, large_tile.rows, large_tile.columns, K), small = tile_count(max_rows, n_seg, small_tile.rows, small_tile.columns, K);
+    if (tile_cost(large, large_tile.rows, large_tile.columns) * (large <= kComputeUnits ? 1.3f : 1.0f) <= 1.6f * tile_cost(small, small_tile.rows, small_tile.columns)) return 0;
     return 4 * small <= 5 * kComputeUnits ? 2 : 1;
 }
 
