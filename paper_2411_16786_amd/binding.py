@@ -326,12 +326,13 @@ class Context:
             self._rows("dx_packed", dx_packed, st, max_rows, d), _ptr(workspace), _stream()))
 
     def moe_combine_backward(self, dy, h_packed, inv, scores, dh_packed, dscores):
-        """Gradient of moe_combine without caches: rows ``dh_packed`` and float ``dscores``."""
+        """Gradient of moe_combine without caches: rows ``dh_packed`` and float ``dscores``.  ``h_packed`` may be a larger batch's buffer."""
         st, f32, T, d = self.torch_dtype, torch.float32, dy.shape[0], self.d
         N = T * self.slots
+        rows = min(N, h_packed.numel() // d)                  # inv names no more
         self._check(lib().moe_combine_backward(
             self._h, self._sized("dy", dy, st, T * d), self._rows("h_packed", h_packed, st, 0, d), self._pairs("inv", inv, N),
-            self._sized("scores", scores, f32, N), T, self._rows("dh_packed", dh_packed, st, h_packed.numel() // d, d),
+            self._sized("scores", scores, f32, N), T, self._rows("dh_packed", dh_packed, st, rows, d),
             self._sized("dscores", dscores, f32, N), _stream()))
 
     def moe_route_backward(self, x, Wg, expert_idx, probs_all, dscores, dprobs, dlogits, dx_packed, inv, dx, dz, dWg, dbg, workspace):

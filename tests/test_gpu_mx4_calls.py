@@ -1,7 +1,9 @@
-"""Calls of the 4-bit experts and the layer's gradients as a program makes them: the timing event."""
+"""Calls of the 4-bit experts and the layer's gradients as a program makes them: the timing event, larger buffers."""
 import pytest
 import torch
 
+import mx4_util as M
+from paper_2411_16786_amd import binding as B
 from test_gpu_layer_gradients import Layer
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +36,21 @@ def test_between_event_is_recorded_between_the_products(call, T):
     run()                                                           # without the hook the event stays as it is
     torch.cuda.synchronize()
     assert before.elapsed_time(between) == first
+
+
+def test_combine_backward_with_buffers_of_a_larger_batch():
+    """Rows of a buffer that was made for more tokens: the gradient needs one for every pair of this batch, not for every row of it."""
+    T, d, k = 9, 64, 2
+    gen = torch.Generator().manual_seed(3)
+    ctx = B.Context(32, d, 64, 4, k, "bf16")
+    _, _, _, perm, inv, R = M.route(gen, T, 4, k, 0.2)
+    dy, h = (torch.randn((n, d), generator=gen).bfloat16().cuda() for n in (T, 32 * k))
+    s = torch.rand((T, k), generator=gen).cuda()
+    dh, ds = torch.full((T * k, d), 3.0, dtype=torch.bfloat16, device="cuda"), torch.empty((T, k), device="cuda")
+    ctx.moe_combine_backward(dy, h, inv.cuda(), s, dh, ds)
+    pair = perm[:R].long()
+    want = s.cpu().flatten()[pair].double()[:, None] * dy.cpu()[pair // k].double()
+    M.within(dh[:R], want, 2.0 ** -8 * want.abs() * (1 + 1e-6) + 2.0 ** -24 * want.abs() + 1e-38, "dh")
+    assert (dh[R:] == 3.0).all()
+    with pytest.raises(ValueError, match="dh_packed"):
+        ctx.moe_combine_backward(dy, h, inv.cuda(), s, dh[:T * k - 1], ds)
