@@ -1,4 +1,4 @@
-"""Calls of the 4-bit experts and the layer's gradients as a program makes them: the timing event, larger buffers."""
+"""Calls of the 4-bit experts and the layer's gradients as a program makes them: the timing event, a stream that is busy, larger buffers."""
 import pytest
 import torch
 
@@ -36,6 +36,42 @@ def test_between_event_is_recorded_between_the_products(call, T):
     run()                                                           # without the hook the event stays as it is
     torch.cuda.synchronize()
     assert before.elapsed_time(between) == first
+
+
+def test_calls_wait_for_a_busy_stream():
+    """Inputs arrive on a side stream behind long work: a call that went to another stream would read the old ones, and find outputs
+    that the side stream fills only then."""
+    L = Layer(64, 128, 256, 4, 2, "bf16", False)
+    x, dy = L.on["x"].clone(), L.on["dy"].clone()
+    outs = lambda: [L.buf.y, L.u, L.dh, L.ds, L.dxp, L.dx, L.dz, L.dWg, L.dbg]
+    L.step()
+    want = [t.clone() for t in outs()]
+    w = torch.randn((64, 128, 256), device="cuda").to(L.dt)
+    codes, scales = (torch.empty(s, dtype=torch.uint8, device="cuda") for s in ((64, 128, 128), (64, 128, 8)))
+    L.ctx.moe_quantize_mx4(w, codes, scales)
+    want += [codes.clone(), scales.clone()]
+    late = w.clone()
+    for t in (L.on["x"], L.on["dy"], w):
+        t.fill_(1.0)
+    a = torch.randn((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    b = torch.empty_like(a)
+    torch.mm(a, a, out=b)
+    torch.cuda.synchronize()
+    side, work = torch.cuda.Stream(), torch.cuda.Event()
+    with torch.cuda.stream(side):
+        for _ in range(40):                                         # some 30 ms; the calls are enqueued within one or two
+            torch.mm(a, a, out=b)
+        work.record()
+        for t in outs() + [codes, scales]:
+            t.fill_(7)
+        for to, value in ((L.on["x"], x), (L.on["dy"], dy), (w, late)):
+            to.copy_(value)
+        L.step()
+        L.ctx.moe_quantize_mx4(w, codes, scales)
+        got = [t.clone() for t in outs() + [codes, scales]]
+    assert not work.query(), "the calls were enqueued too late to show anything"
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
 def test_combine_backward_with_buffers_of_a_larger_batch():
