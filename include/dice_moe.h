@@ -112,7 +112,9 @@ int moe_destroy(moe_ctx* ctx);
  * use for T_max tokens: the FFN's hidden activations [T_max*k, F], (MOE_BF16) 28 MB of float
  * partial sums for the second GEMM when its reduction is split over several workgroups (few
  * rows), and the status words of moe_expert_ffn_status.  moe_expert_ffn_mx4 and its gradient keep their
- * hidden activations and moe_route_backward its partial sums in the same place.  One workspace can serve all three calls of a layer, and all layers, on one stream. */
+ * hidden activations in the same place, moe_route_backward its partial sums in all that is ahead of the status words (only
+ * contexts with few F and many E * d are asked for more because of it).  One workspace can serve all calls of a layer, and
+ * all layers, on one stream. */
 size_t moe_workspace_bytes(const moe_ctx* ctx);
 
 /* Text of the last error recorded on this context ("" if none); valid until the next call. */

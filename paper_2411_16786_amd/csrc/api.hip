@@ -46,16 +46,16 @@ size_t hidden_bytes(const moe_ctx* ctx)
 }
 
 // the two status words of the FFN's launch check sit behind the hidden activations and the partial sums
-// (the dispatch scratch and the partial sums of moe_route_backward share the start of the workspace with the
-// hidden activations: the calls of one workspace run in stream order)
+// (the dispatch scratch shares the start of the workspace with the hidden activations, the partial sums of
+// moe_route_backward all that is ahead of the status words: the calls of one workspace run in stream order)
 size_t status_offset(const moe_ctx* ctx)
 {
     size_t front = hidden_bytes(ctx);
     const size_t disp = dicemoe::dispatch_scratch_bytes(static_cast<long long>(ctx->shape.T_max) * slots(ctx), experts(ctx));
     if (disp > front) front = (disp + 255) / 256 * 256;
-    const size_t route = dicemoe::route_backward_bytes(ctx->shape.T_max, ctx->shape.E, ctx->shape.d);
-    if (route > front) front = (route + 255) / 256 * 256;
-    return front + (is_bf16(ctx) ? dicemoe::kSplitKBytes : 0);
+    front += is_bf16(ctx) ? dicemoe::kSplitKBytes : 0;
+    const size_t route = dicemoe::route_backward_bytes(is_bf16(ctx), ctx->shape.T_max, ctx->shape.E, ctx->shape.d);
+    return route > front ? (route + 255) / 256 * 256 : front;
 }
 
 int check_T(moe_ctx* ctx, int32_t T)

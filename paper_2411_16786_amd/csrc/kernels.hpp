@@ -115,7 +115,7 @@ hipError_t launch_combine_backward(bool bf16, const void* dy, const void* h_pack
                                    int d, int k, void* dh_packed, float* dscores, hipStream_t stream);
 
 // Gradient of router and dispatch (Wg null: of the dispatch alone).  slots: columns of idx, dscores and inv, the first k of them routed.
-// partial, partial_dbg (and dz, where it is null): set by the launcher, in a workspace of route_backward_bytes(T, E, d) bytes.
+// partial, partial_dbg (and dz, where it is null): set by the launcher, in a workspace of route_backward_bytes(bf16, T_max, E, d) bytes.
 struct RouteBackward {
     const void *x, *Wg;
     const int32_t* idx;
@@ -127,7 +127,7 @@ struct RouteBackward {
     int T, d, E, k, slots, renorm;
     float *partial, *partial_dbg;
 };
-size_t route_backward_bytes(long long T_max, int E, int d);
+size_t route_backward_bytes(bool bf16, long long T_max, int E, int d);
 hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hipStream_t stream);
 
 hipError_t launch_ep_segments(const int32_t* recv_counts, int n_seg, int E_loc, int32_t* seg_offsets,

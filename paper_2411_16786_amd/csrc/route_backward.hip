@@ -7,6 +7,7 @@
 #include <type_traits>
 #include "common.hpp"
 #include "kernels.hpp"
+#include "route_plan.hpp"
 
 namespace dicemoe {
 
@@ -327,21 +328,6 @@ __global__ __launch_bounds__(256) void route_backward_sum_kernel(const float* __
 
 namespace {
 
-// Tokens per workgroup: 64, one tile per wavefront, and up to 256 (128 with more than 32 experts, whose dz has to fit the LDS) while that
-// leaves two workgroups per compute unit, which keeps the partial sums a small part of what is read; with more than 32 chunks, whose
-// sum takes long, also while it leaves one (8 experts, 4096 tokens of 1152 columns, 64 and 32 chunks: 16.1 + 7.5 and 16.0 + 4.2 us; 16
-// experts, 8192 of 1792, 64 and 32: 34.9 + 7.8 and 32.4 + 4.8; 4096 of 2048, 32 and 16: 19.2 + 4.2 and 20.5 + 4.0).
-int route_chunk(int T_tok, int E, int columns)
-{
-    int chunk = 64;
-    while (chunk < (E > 32 ? 128 : 256)) {
-        const int least = (T_tok + chunk - 1) / chunk > 32 ? kComputeUnits : 2 * kComputeUnits;
-        if (static_cast<long long>((T_tok + 2 * chunk - 1) / (2 * chunk)) * columns < least) break;
-        chunk *= 2;
-    }
-    return chunk;
-}
-
 template <typename T, int NB>
 void launch_route_backward_t(const RouteBackward& a, int columns, int chunk, int chunks, hipStream_t stream)
 {
@@ -374,10 +360,13 @@ void launch_dispatch_backward_t(const RouteBackward& a, hipStream_t stream)
 
 }  // namespace
 
-// partial sums by chunks of 64 tokens or more, and dz if the caller does not want it
-size_t route_backward_bytes(long long T_max, int E, int d)
+static int route_columns(bool bf16, int d) { return (d + (bf16 ? 128 : 64) - 1) / (bf16 ? 128 : 64); }       // 16 x kVec columns each
+
+// partial sums by chunks of tokens, and dz if the caller does not want it
+size_t route_backward_bytes(bool bf16, long long T_max, int E, int d)
 {
-    return (static_cast<size_t>((T_max + 63) / 64) * E * (static_cast<size_t>(d) + 1) + static_cast<size_t>(T_max) * E) * sizeof(float);
+    const size_t chunks = static_cast<size_t>(route_chunks_most(T_max, E, route_columns(bf16, d)));
+    return (chunks * E * (static_cast<size_t>(d) + 1) + static_cast<size_t>(T_max) * E) * sizeof(float);
 }
 
 hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hipStream_t stream)
@@ -388,7 +377,7 @@ hipError_t launch_route_backward(bool bf16, RouteBackward a, void* workspace, hi
         else launch_dispatch_backward_t<float>(a, stream);
         return hipGetLastError();
     }
-    const int V = bf16 ? 8 : 4, columns = (a.d + 16 * V - 1) / (16 * V);
+    const int columns = route_columns(bf16, a.d);
     const int chunk = route_chunk(a.T, a.E, columns), chunks = (a.T + chunk - 1) / chunk;
     a.partial = static_cast<float*>(workspace);
     a.partial_dbg = a.partial + static_cast<size_t>(chunks) * a.E * a.d;

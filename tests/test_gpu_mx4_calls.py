@@ -1,4 +1,4 @@
-"""Calls of the 4-bit experts and the layer's gradients as a program makes them: the timing event, a stream that is busy, larger buffers."""
+"""Calls of the 4-bit experts and the layer's gradients as a program makes them: the timing event, a stream that is busy, larger buffers, the workspace's end."""
 import pytest
 import torch
 
@@ -90,3 +90,28 @@ def test_combine_backward_with_buffers_of_a_larger_batch():
     assert (dh[R:] == 3.0).all()
     with pytest.raises(ValueError, match="dh_packed"):
         ctx.moe_combine_backward(dy, h, inv.cuda(), s, dh[:T * k - 1], ds)
+
+
+@pytest.mark.parametrize("T_max,d,E,k,dtype", [(4096, 1024, 64, 1, "bf16"), (4096, 64, 64, 2, "f32"), (2000, 2048, 33, 1, "bf16"), (300, 64, 8, 1, "bf16")])
+def test_router_gradient_stays_in_the_workspace(T_max, d, E, k, dtype):
+    """A context whose workspace is the partial sums of this call: what lies behind it stays, at every number of tokens."""
+    ctx, dt = B.Context(T_max, d, 64, E, k, dtype), M.DT[dtype]
+    size = ctx.workspace_bytes()
+    ws = torch.full((size + (1 << 20),), 171, dtype=torch.uint8, device="cuda")
+    gen = torch.Generator().manual_seed(T_max)
+    for T in (1, 63, 64, 129, 1000, 2047, 2048, 2049, 4096):
+        if T > T_max:
+            break
+        print("T", T, flush=True)
+        P = torch.softmax(torch.randn((T, E), generator=gen), 1)
+        idx = torch.topk(P, k, 1).indices.to(torch.int32)
+        x, Wg = torch.randn((T, d), generator=gen).to(dt), torch.randn((E, d), generator=gen).to(dt)
+        ds = torch.randn((T, k), generator=gen)
+        dx, dWg, dbg = torch.empty((T, d), dtype=dt, device="cuda"), torch.empty((E, d), device="cuda"), torch.empty(E, device="cuda")
+        ctx.moe_route_backward(x.cuda(), Wg.cuda(), idx.cuda(), P.cuda(), ds.cuda(), None, None, None, None, dx, None, dWg, dbg, ws[:size])
+        g = torch.zeros((T, E), dtype=torch.float64).scatter_add(1, idx.long(), ds.double())
+        dz = P.double() * (g - (P.double() * g).sum(1, keepdim=True))
+        off = (E + k + 8) * 2.0 ** -24 * (P.double() * (g.abs() + (P.double() * g.abs()).sum(1, keepdim=True)))
+        M.within(dWg, dz.T @ x.double(), (T + 8) * 2.0 ** -23 * (dz.abs().T @ x.double().abs()) + off.T @ x.double().abs() + 1e-38, "dWg")
+        M.within(dbg, dz.sum(0), (T + 8) * 2.0 ** -24 * dz.abs().sum(0) + off.sum(0) + 1e-38, "dbg")
+    assert (ws[size:] == 171).all()
