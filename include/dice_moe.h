@@ -261,7 +261,7 @@ int moe_expert_ffn_commit(moe_ctx* ctx, const void* x_rows, const int32_t* row_p
                           const float* scores, const uint8_t* mask, int32_t T, void* H_buffer,
                           float* S_buffer, void* workspace, void* stream);
 
-/* Launch check of the expert FFN calls.  Segment sizes live on the device, so the three calls above
+/* Launch check of the expert FFN calls.  Segment sizes live on the device, so the three calls above, moe_expert_ffn_mx4 and its gradient
  * size their launch from the host bound max_rows; if the segment table holds more rows than that,
  * the rows beyond the launched tiles are NOT computed.  Every FFN call records the comparison in
  * its workspace; this call waits for `stream` (it is the one entry point that synchronises the
@@ -362,8 +362,10 @@ int moe_quantize_mx4(moe_ctx* ctx, const void* W, int64_t rows, int32_t cols, ui
 /* moe_expert_ffn on 4-bit weights: u = W1_e . x + b1_e, h = W2_e . gelu(u) + b2_e for every row of every segment.  The weights
  * are exact in the products (a code with its scale is a bf16 value, or infinite from 2^128 on); sums are float, and gelu(u) is rounded to dtype once.
  *   in : x_rows: packed rows (row_pairs NULL) or x[T][d] read through row_pairs as in moe_expert_ffn_rows;
- *        out_pairs: NULL, or the row of h_rows that packed row r goes to (distinct), as in moe_expert_ffn_commit: with
- *        moe_dispatch's perm and h_rows = H_cache, moe_combine with h_packed = NULL follows;
+ *        out_pairs: NULL, or the row of h_rows that packed row r goes to (distinct): with
+ *        moe_dispatch's perm and h_rows = H_cache, moe_combine with h_packed = NULL follows, as after moe_expert_ffn_commit
+ *        without scores.  There are no scores, mask and S_buffer here: the asynchronous schedules, which commit the scores with the rows,
+ *        have no form on 4-bit weights, nor has moe_layer_forward;
  *        seg_offsets, seg_expert, n_segments, max_rows, b1, b2 as in moe_expert_ffn.  Packed rows from max_rows on are not
  *        touched (moe_expert_ffn_status reports that there were some), nor are segments whose expert is out of range
  *   out: h_rows (dtype); u_packed[..][F] (dtype, may be NULL): the pre-activations by packed row, for the gradient
