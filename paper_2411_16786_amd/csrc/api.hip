@@ -189,7 +189,8 @@ int check_ffn(moe_ctx* ctx, const char* who, const void* x_rows, const int32_t* 
 }
 
 // The 4-bit expert FFN calls: whole scale groups in every weight row, offsets inside one expert's codes well within 64 bits, and less
-// than the 2^32 threads that a launch holds (the kernels of few rows have most: 512 for 16 rows and 32 columns)
+// than the 2^32 threads that a launch holds: 512 for 16 rows and 32 columns is the most of any kernel whose grid grows with the sizes.  (Two
+// forms for few rows have more per column, 512 for 16 columns and 1024 for 32, but the plan takes them for at most 1536 and 512 workgroups.)
 int check_mx4(moe_ctx* ctx, const char* who, int32_t n_segments, int32_t max_rows)
 {
     const moe_shape& s = ctx->shape;

@@ -1,8 +1,12 @@
 // Expert FFN on 4-bit weights (mx4.hpp), forward and gradient of its rows, as grouped products over segments of rows.
 //   forward : u = x W1_e^T + b1_e,   h = gelu(u) W2_e^T + b2_e        (gelu(u) rounded to the storage type once)
 //   gradient: du = (dh W2_e) gelu'(u),   dx = du W1_e                 (du rounded to the storage type once)
+// In bf16 those two roundings are the matrix instructions' own: what the second product reads is a bf16 operand, as in the FFN on bf16
+// weights; two bf16 parts for each value would double its products.  They raise the distance of h and dx from the exact result from
+// 0.0017 of its size, the last rounding's, to 0.0023.  (du is rounded whether or not the caller keeps it: dx has the same bits.)
 // The weights are the first operand of the matrix instructions and the rows the second, so a result register holds four
-// output columns of one row.  Weights go from memory to the instruction through registers alone, converted on the way.
+// output columns of one row.  The kernels for few rows below take the weights from memory to the instruction through registers alone, converted
+// on the way; the tiles for many rows (mx4_tile.hpp, mx4_tile_t.hpp) stage codes and scales through LDS.
 #include <type_traits>
 #include "ffn_mfma.hpp"
 #include "kernels.hpp"
@@ -55,8 +59,10 @@ __global__ __launch_bounds__(KS * kWave) void mx4_rows_kernel(const T* __restric
     f32x4_t acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // AHEAD: what the next step needs is under way behind this one's products (one token, 4608 -> 1152 6.0 us against 6.6; with two
-    // sets of weights the registers cost more, eight tokens 1152 -> 4608 11.2 against 8.8)
+    // AHEAD: what the next step needs is under way behind this one's products (one token, 4608 -> 1152 6.0 us against 6.6).  With two sets
+    // of weights the registers cost more where a wavefront has one or two steps (16 rows over 8 experts, 1152 -> 4608 9.4 against 7.4; 26 over
+    // 16, 2048 -> 8192 46.6 against 39.5); with eight steps, 8192 -> 2048, 16 rows take 32.1 against 31.1, 26 rows 41.6 against 45.2 and 40 rows
+    // 43.6 against 47.7, which is left as it is
     constexpr bool AHEAD = NT == 1;
     u32x4_t c_next[NT], x_next[XV];
     uint32_t s_next[NT];

@@ -54,6 +54,10 @@ inline bool rows_wide(int max_rows, int n_seg, int N) { return tile_bound(max_ro
 // rates of 8192 -> 4096 of 8192 rows (444, 481 and 563 us; the tiles of 32 rows are for few rows); a compute unit with a single workgroup
 // of four wavefronts waits more.  Of the two of 32 rows, in shares, the narrower one in more shares while each tile has a compute unit
 // to itself (200 rows over 8 experts: 4608 -> 1152 13.4 us against 21.8, 1152 -> 4608, 288 tiles, 16.6 against 12.6).
+// The factors 1.3 (that single workgroup) and 2.5 (tiles of 32 rows) over both products of 100 to 8192 rows, 1152 -> 4608 over 8 experts,
+// 384 -> 1536 and 2048 -> 8192 over 16: the tile taken is 2.2 % above the fastest on average.  1 in place of 1.3: 3.1 % (2000 rows, 4608 -> 1152 44
+// us against 35; 8192 rows, 1536 -> 384 18.6 against 16.3; the other way 1000 rows, 8192 -> 2048 76 against 85).  1.8 in place of 2.5: 2.6 % (400
+// rows, 2048 -> 8192 53 against 44), 3: 3.0 % (200 rows, 1152 -> 4608 14.0 against 12.0); 2.1, which is their rate, takes the same tiles.
 // Tiles of 64 rows in two shares while there are no more than 5/4 per compute unit (4608 -> 1152 over 8 experts, 1000 rows 29 us against
 // 35.5, 2000 rows, 315 tiles, 39 both; 300 rows over 16 experts, 8192 -> 2048, 53 against 62.5).
 inline int pick_tile(int max_rows, int n_seg, int N, int K)
@@ -77,8 +81,11 @@ inline int pick_tile(int max_rows, int n_seg, int N, int K)
 }
 
 // The same for mx4_tile_transposed_kernel (32 RT rows x 64 WN columns of K; its LDS does not depend on the reduction).  4608 -> 1152, 8192
-// rows 64 x 256 tiles 108 us, 32 x 128 in two shares 165; 2000 rows 70 and 46, in four shares 51; 400 rows 57, 30 and 23, 1000 rows (315
-// tiles, 320 being 5/4 per compute unit) two shares 36, four 30.  1152 -> 4608, 2000 rows 43 and 57, 400 rows 23, 20 and in four shares 30.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
+// rows 64 x 256 tiles 100 us, 32 x 128 in two shares 129; 2000 rows 57 and 43, in four shares 48; 400 rows 56, 30 and 23, 1000 rows (315
+// tiles, 320 being 5/4 per compute unit) two shares 33, four 27.  1152 -> 4608, 2000 rows 38 and 54, 400 rows 24, 20 and in four shares 31.  Rows in sixteens, two rows a segment: 11.6 us against 14.9 in four shares.
+// 1.3 as above, and 1.6 by which a 32-row tile takes longer by area: over the same products the tile taken is 2.0 % above the fastest; 1 in
+// place of 1.3 4.0 % (2000 rows, 4608 -> 1152 57 us against 43), 1.3 in place of 1.6 3.8 % (4000 rows, 8192 -> 2048 243 against 180), 2 3.8 %
+// (1000 rows, 8192 -> 2048 131 against 93).
 constexpr int kTilesT = 3;
 constexpr TileSize kTileT[kTilesT] = {{64, 256, 1}, {32, 128, 2}, {32, 128, 4}};
 inline int pick_tile_t(int max_rows, int n_seg, int K)

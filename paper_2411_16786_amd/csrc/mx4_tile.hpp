@@ -9,10 +9,14 @@
 //
 // Direct-to-LDS loads, two stages of rows and two pairs of stages of codes in the LDS: what a stage has left is asked for again behind
 // its barrier, which stands before the stage's last slice, so that barrier and first reads of the next stage lie behind matrix
-// instructions.  What bounds it is the instruction stream between matrix instructions and the wait for the next stage; more wavefronts
-// per SIMD hide both, which is why the rings are short.  8192 rows over 8 experts (us; this library's bf16 GEMMs take 105 with GELU
-// and 92): 1152 -> 4608 with GELU, 256 x 128 tiles 91, 128 x 128 102, 128 x 64 100; 4608 -> 1152, 128 x 64 93, 128 x 128 92,
-// 256 x 128 103.  Rings of three stages, one workgroup less per compute unit: 113, 101, 105 and 103, 123, 115.  Stages through
+// instructions.  What takes the time there, by counters over 8192 rows and 8 experts, 1152 -> 4608 and 4608 -> 1152: the matrix pipes are
+// busy 47 and 42 % of the cycles, a wavefront waits 37 and 45 % of its time for a stage or at a barrier and 38 and 26 % to issue; more wavefronts
+// per SIMD hide both, which is why the rings are short.  That is not the limit of the instruction stream: at 8192 -> 4096, 128 stages a tile
+// instead of 18, the widest tile holds 1.24 PFLOP/s against 0.98 at 1152 -> 4608.  What differs is the start and the epilogue of a tile, paid every 18
+// stages, and a last round of workgroups that is partly filled (1152 tiles and more on the 512 places of two a compute unit).
+// 8192 rows over 8 experts (us, medians of 54 calls; this library's bf16 GEMMs take 105 with GELU
+// and 92): 1152 -> 4608 with GELU, 256 x 128 tiles 89, 128 x 128 108, 128 x 64 101; 4608 -> 1152, 128 x 64 91, 128 x 128 92,
+// 256 x 128 102.  Rings of three stages, one workgroup less per compute unit: 113, 101, 105 and 103, 123, 115.  Stages through
 // registers: 110 and 122 at best.
 #pragma once
 #include <type_traits>

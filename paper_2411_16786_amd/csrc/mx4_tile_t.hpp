@@ -9,8 +9,10 @@
 // slice's come with two broadcast reads.
 // A workgroup of WN wavefronts owns BK = 64 WN columns of BR = 32 RT rows, a wavefront 64 columns: of its two blocks, block i has the
 // columns 2 c + i.  Stages of 64 n, two in the LDS, barrier ahead of the last slice as there.
-// Bound by the conversions and permutations beside the matrix instructions.  8192 rows over 8 experts, 64 x 256 tiles: 4608 -> 1152 106 to
-// 118 us, 1152 -> 4608 with the slope 122 to 134 (0.74 to 0.82 and 0.65 to 0.71 PFLOP/s).
+// By counters over 8192 rows and 8 experts, 64 x 256 tiles, 4608 -> 1152 and 1152 -> 4608 with the slope: matrix pipes busy 37 and 32 % of the
+// cycles, a wavefront waits 42 and 41 % of its time for a stage or at a barrier, 31 and 33 % to issue (the conversions and permutations beside
+// the matrix instructions).  Medians: 104 and 119 us (0.83 and 0.73 PFLOP/s) on one set of rows and two of weights, 114 and 134 (0.76 and 0.65)
+// over three sets of everything, which do not fit the memory-side cache.
 #pragma once
 #include "mx4_tile.hpp"
 
