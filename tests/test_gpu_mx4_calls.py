@@ -59,7 +59,7 @@ def test_calls_wait_for_a_busy_stream():
     torch.cuda.synchronize()
     side, work = torch.cuda.Stream(), torch.cuda.Event()
     with torch.cuda.stream(side):
-        for _ in range(40):                                         # some 30 ms; the calls are enqueued within one or two
+        for _ in range(100):                                        # some 75 ms; the calls are enqueued within one or two
             torch.mm(a, a, out=b)
         work.record()
         for t in outs() + [codes, scales]:
